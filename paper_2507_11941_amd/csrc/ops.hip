@@ -1,0 +1,270 @@
+// Host side of include/bpe_ops.h: argument checks and the enqueue of the operators on token batches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstddef>
+
+#include "../../include/bpe_ops.h"
+#include "embed_kernels.h"
+#include "logits_kernels.h"
+
+using namespace bpe;
+
+namespace {
+
+int launched() { return hipGetLastError() == hipSuccess ? BPE_OK : BPE_EHIP; }
+
+size_t size_of(int dtype) { return dtype == BPE_F32 ? 4 : 2; }
+
+bool is_type(int dtype) { return dtype == BPE_F32 || dtype == BPE_BF16 || dtype == BPE_F16; }
+
+// Whether p may be used for n values of `size` bytes.
+bool fits(const void* p, int64_t n, size_t size) { return (n == 0 || p) && ((uintptr_t)p & (size - 1)) == 0; }
+
+// ... and, if there is one, an optional array.
+bool aligned(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) == 0; }
+
+bool is_matrix(const void* p, int dtype, int64_t rows, int64_t columns, int64_t stride) {
+  return is_type(dtype) && columns >= 1 && columns <= BPE_MAX_COLUMNS && stride >= columns && stride < ((int64_t)1 << 40) &&
+         fits(p, rows, size_of(dtype));
+}
+
+bool is_count(int64_t n) { return n >= 0 && n <= BPE_MAX_TOKENS; }
+
+bool is_workspace(const void* p, size_t bytes, size_t need) { return p && ((uintptr_t)p & 255) == 0 && bytes >= need && need > 0; }
+
+unsigned blocks(int64_t n, int64_t each) { return (unsigned)((n + each - 1) / each); }
+
+// Calls f with a value of the type.
+template <typename F>
+void with_type(int dtype, F&& f) {
+  if (dtype == BPE_F32) f(float{});
+  else if (dtype == BPE_BF16) f(bf16{});
+  else f(f16{});
+}
+
+size_t place(size_t& total, size_t bytes) {
+  const size_t at = total;
+  total += (bytes + 255) & ~(size_t)255;
+  return at;
+}
+
+// The parts of the workspace of the functions on logits.
+struct LogitsWorkspace {
+  size_t logprobs, values, upstream, advantage, counts, total;
+};
+
+LogitsWorkspace logits_layout(int64_t n, int32_t batch) {
+  LogitsWorkspace w{};
+  w.logprobs = place(w.total, (size_t)n * 8);
+  w.values = place(w.total, (size_t)std::max<int64_t>(n, batch) * 8);
+  w.upstream = place(w.total, (size_t)n * 4);
+  w.advantage = place(w.total, (size_t)n * 4);
+  w.counts = place(w.total, ((size_t)batch + 1) * 4);
+  return w;
+}
+
+template <typename T>
+void launch_grad(const T* logits, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets, const float* lse,
+                 const float* upstream, T* grad, int64_t grad_stride, hipStream_t stream) {
+  hipLaunchKernelGGL(logprobs_grad_kernel<T>, dim3((unsigned)n), dim3(256), 0, stream, logits, vocab, stride, targets, lse,
+                     upstream, grad, grad_stride);
+}
+
+}  // namespace
+
+extern "C" {
+
+int bpe_embed_tokens(const void* weight, int dtype, int64_t vocab, int64_t dim, int64_t weight_stride, const int32_t* ids,
+                     int64_t n, const int64_t* count, float scale, void* out, int64_t out_stride, void* stream) {
+  if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS || !is_matrix(weight, dtype, vocab, dim, weight_stride) ||
+      !is_matrix(out, dtype, n, dim, out_stride) || !fits(ids, n, 4) || !aligned(count, 8))
+    return BPE_EINVAL;
+  if (n == 0) return BPE_OK;
+  with_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    hipLaunchKernelGGL(embed_kernel<T>, dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream, (const T*)weight, vocab, dim,
+                       weight_stride, ids, n, count, scale, (T*)out, out_stride);
+  });
+  return launched();
+}
+
+size_t bpe_embed_tokens_grad_workspace_bytes(int64_t n, int64_t vocab, int64_t dim) {
+  if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS || dim < 1 || dim > BPE_MAX_COLUMNS) return 0;
+  return 256;
+}
+
+int bpe_embed_tokens_grad(const void* grad, int dtype, int64_t grad_stride, const int32_t* ids, int64_t n,
+                          const int64_t* count, int64_t vocab, int64_t dim, float scale, int accumulate, void* grad_weight,
+                          int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS || !is_matrix(grad, dtype, n, dim, grad_stride) ||
+      !is_matrix(grad_weight, out_dtype, vocab, dim, out_stride) || (out_dtype != dtype && out_dtype != BPE_F32) ||
+      !fits(ids, n, 4) || !aligned(count, 8) ||
+      !is_workspace(workspace, workspace_bytes, bpe_embed_tokens_grad_workspace_bytes(n, vocab, dim)))
+    return BPE_EINVAL;
+  with_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    const auto launch = [&](auto out_type) {
+      using O = decltype(out_type);
+      hipLaunchKernelGGL((embed_grad_kernel<T, O>), dim3((unsigned)vocab), dim3(256), 0, (hipStream_t)stream, (const T*)grad,
+                         grad_stride, ids, n, count, dim, scale, accumulate, (O*)grad_weight, out_stride);
+    };
+    if (out_dtype == BPE_F32) launch(float{});
+    else launch(type);
+  });
+  return launched();
+}
+
+int bpe_next_tokens(const int32_t* ids, int64_t n, const int64_t* offsets, int32_t batch, const int32_t* first,
+                    int32_t* targets, void* stream) {
+  if (!is_count(n) || batch < 0 || !fits(ids, n, 4) || !offsets || !aligned(offsets, 8) || !aligned(first, 4) ||
+      !fits(targets, n, 4))
+    return BPE_EINVAL;
+  if (n == 0) return BPE_OK;
+  hipLaunchKernelGGL(next_tokens_kernel, dim3(blocks(n, 256)), dim3(256), 0, (hipStream_t)stream, ids, n, offsets, batch, first,
+                     targets);
+  return launched();
+}
+
+size_t bpe_logits_workspace_bytes(int64_t n, int64_t vocab, int32_t batch) {
+  if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS || batch < 0) return 0;
+  return logits_layout(n, batch).total;
+}
+
+int bpe_token_logprobs(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets,
+                       float* logprobs, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!is_count(n) || !is_matrix(logits, dtype, n, vocab, stride) || !fits(targets, n, 4) || !aligned(logprobs, 4) ||
+      !aligned(lse, 4) || !is_workspace(workspace, workspace_bytes, bpe_logits_workspace_bytes(n, vocab, 0)))
+    return BPE_EINVAL;
+  if (n == 0) return BPE_OK;
+  RowArgs a{};
+  a.targets = targets;
+  a.logprobs = logprobs;
+  a.lse = lse;
+  with_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    hipLaunchKernelGGL((row_kernel<T, kRowLogprob>), dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream, (const T*)logits,
+                       vocab, stride, a, (T*)nullptr);
+  });
+  return launched();
+}
+
+int bpe_token_logprobs_grad(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets,
+                            const float* lse, const float* upstream, void* grad, int64_t grad_stride, void* stream) {
+  if (!is_count(n) || !is_matrix(logits, dtype, n, vocab, stride) || !is_matrix(grad, dtype, n, vocab, grad_stride) ||
+      !fits(targets, n, 4) || !fits(lse, n, 4) || !fits(upstream, n, 4))
+    return BPE_EINVAL;
+  if (n == 0) return BPE_OK;
+  with_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    launch_grad((const T*)logits, n, vocab, stride, targets, lse, upstream, (T*)grad, grad_stride, (hipStream_t)stream);
+  });
+  return launched();
+}
+
+int bpe_token_logprobs_and_grad(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride,
+                                const int32_t* targets, const float* upstream, float* logprobs, float* lse, void* grad,
+                                int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!is_count(n) || !is_matrix(logits, dtype, n, vocab, stride) || !is_matrix(grad, dtype, n, vocab, grad_stride) ||
+      !fits(targets, n, 4) || !fits(upstream, n, 4) || !aligned(logprobs, 4) || !aligned(lse, 4) ||
+      !is_workspace(workspace, workspace_bytes, bpe_logits_workspace_bytes(n, vocab, 0)))
+    return BPE_EINVAL;
+  if (n == 0) return BPE_OK;
+  RowArgs a{};
+  a.targets = targets;
+  a.logprobs = logprobs;
+  a.lse = lse;
+  a.upstream = upstream;
+  a.grad_stride = grad_stride;
+  with_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    hipLaunchKernelGGL((row_kernel<T, kRowStep>), dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream, (const T*)logits, vocab,
+                       stride, a, (T*)grad);
+  });
+  return launched();
+}
+
+int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets,
+                        const int64_t* offsets, int32_t batch, const float* reference, float beta, float smoothing,
+                        float scale, float* loss, float* margins, float* logprobs, void* grad, int64_t grad_stride,
+                        void* workspace, size_t workspace_bytes, void* stream_ptr) {
+  if (!is_count(n) || !is_matrix(logits, dtype, n, vocab, stride) || !is_matrix(grad, dtype, n, vocab, grad_stride) ||
+      batch < 0 || batch % 2 || !fits(targets, n, 4) || !offsets || !aligned(offsets, 8) || !aligned(reference, 4) ||
+      !std::isfinite(beta) || !(smoothing >= 0.0f && smoothing <= 1.0f) || !std::isfinite(scale) || !loss || !aligned(loss, 4) ||
+      !aligned(margins, 4) || !aligned(logprobs, 4) ||
+      !is_workspace(workspace, workspace_bytes, bpe_logits_workspace_bytes(n, vocab, batch)))
+    return BPE_EINVAL;
+  const LogitsWorkspace w = logits_layout(n, batch);
+  const hipStream_t stream = (hipStream_t)stream_ptr;
+  char* ws = (char*)workspace;
+  double* lp = (double*)(ws + w.logprobs);
+  double* losses = (double*)(ws + w.values);
+  float* upstream = (float*)(ws + w.upstream);
+  float* lse = (float*)(ws + w.advantage);
+  RowArgs a{};
+  a.targets = targets;
+  a.logprobs = logprobs;
+  a.logprobs64 = lp;
+  a.lse = lse;
+  with_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    if (n > 0) {
+      hipLaunchKernelGGL((row_kernel<T, kRowLogprob>), dim3((unsigned)n), dim3(256), 0, stream, (const T*)logits, vocab, stride,
+                         a, (T*)nullptr);
+      hipLaunchKernelGGL(zero_kernel, dim3(blocks(n, 256)), dim3(256), 0, stream, upstream, n);
+    }
+    if (batch > 0)
+      hipLaunchKernelGGL(pair_kernel, dim3(batch / 2), dim3(256), 0, stream, lp, targets, n, vocab, offsets, batch, reference,
+                         beta, smoothing, scale, margins, losses, upstream);
+    hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(256), 0, stream, losses, (int64_t)(batch / 2), loss);
+    if (n > 0)
+      launch_grad((const T*)logits, n, vocab, stride, targets, lse, upstream, (T*)grad, grad_stride, stream);
+  });
+  return launched();
+}
+
+int bpe_policy_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets,
+                    const int64_t* offsets, int32_t batch, const float* old, const float* advantages,
+                    int advantage_by_string, const float* reference, float clip_low, float clip_high, float kl_weight,
+                    int by_string, float scale, float* loss, float* logprobs, void* grad, int64_t grad_stride,
+                    void* workspace, size_t workspace_bytes, void* stream_ptr) {
+  if (!is_count(n) || !is_matrix(logits, dtype, n, vocab, stride) || !is_matrix(grad, dtype, n, vocab, grad_stride) ||
+      batch < 0 || !fits(targets, n, 4) || !offsets || !aligned(offsets, 8) || !fits(old, n, 4) ||
+      !fits(advantages, advantage_by_string ? batch : n, 4) || !aligned(reference, 4) || !(clip_low >= 0.0f && clip_low <= 1.0f) ||
+      !(clip_high >= 0.0f && std::isfinite(clip_high)) || !(kl_weight >= 0.0f && std::isfinite(kl_weight)) || !std::isfinite(scale) ||
+      !loss || !aligned(loss, 4) || !aligned(logprobs, 4) ||
+      !is_workspace(workspace, workspace_bytes, bpe_logits_workspace_bytes(n, vocab, batch)))
+    return BPE_EINVAL;
+  const LogitsWorkspace w = logits_layout(n, batch);
+  const hipStream_t stream = (hipStream_t)stream_ptr;
+  char* ws = (char*)workspace;
+  int32_t* counts = (int32_t*)(ws + w.counts);
+  RowArgs a{};
+  a.targets = targets;
+  a.logprobs = logprobs;
+  a.grad_stride = grad_stride;
+  a.weight = (float*)(ws + w.upstream);
+  a.advantage = (float*)(ws + w.advantage);
+  a.old = old;
+  a.reference = reference;
+  a.low = clip_low;
+  a.high = clip_high;
+  a.kl_weight = kl_weight;
+  a.scale = scale;
+  a.value = (double*)(ws + w.values);
+  if (n > 0) {
+    hipLaunchKernelGGL(count_kernel, dim3(1), dim3(256), 0, stream, targets, n, vocab, offsets, batch, counts);
+    hipLaunchKernelGGL(weights_kernel, dim3(blocks(n, 256)), dim3(256), 0, stream, targets, n, vocab, offsets, batch, counts,
+                       by_string, advantages, advantage_by_string, (float*)(ws + w.upstream), (float*)(ws + w.advantage));
+    with_type(dtype, [&](auto type) {
+      using T = decltype(type);
+      hipLaunchKernelGGL((row_kernel<T, kRowPolicy>), dim3((unsigned)n), dim3(256), 0, stream, (const T*)logits, vocab, stride, a,
+                         (T*)grad);
+    });
+  }
+  hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(256), 0, stream, a.value, n, loss);
+  return launched();
+}
+
+}  // extern "C"

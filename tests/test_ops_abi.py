@@ -1,0 +1,99 @@
+"""include/bpe_ops.h: the library exports what it declares, and refuses bad arguments before it touches a device."""
+import os
+import re
+
+import paper_2507_11941_amd as bpe
+from paper_2507_11941_amd import _ops
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+EINVAL = -1
+A = 1 << 20                                              # an address that is aligned to everything and never followed
+
+
+def test_library_exports_every_declared_symbol():
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "bpe_ops.h")).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(bpe_[a-z_0-9]+)\s*\(", text)))
+    assert len(names) == 10
+    for name in names:
+        assert hasattr(bpe.load_library(), name), name
+
+
+def call(name, good, bad):
+    """Whether each of the changes `bad` ({argument: value}) of the arguments `good` is refused."""
+    function = getattr(_ops._load(), "bpe_" + name)
+    for at, value in bad:
+        args = list(good.values())
+        args[list(good).index(at)] = value
+        assert function(*args) == EINVAL, (name, at, value)
+
+
+BIG = 1 << 40
+LOGITS = dict(logits=A, dtype=1, n=4, vocab=7, stride=7, targets=A)
+BAD_LOGITS = [("logits", None), ("logits", A + 1), ("dtype", 3), ("dtype", -1), ("n", -1), ("n", BIG), ("vocab", 0), ("vocab", BIG),
+              ("stride", 6), ("stride", BIG), ("targets", None), ("targets", A + 2)]
+WORK = dict(workspace=A, workspace_bytes=1 << 20, stream=None)
+BAD_WORK = [("workspace", None), ("workspace", A + 128), ("workspace_bytes", 0)]
+BAD_GRAD = [("grad", None), ("grad", A + 1), ("grad_stride", 6)]
+
+
+def test_embedding_arguments():
+    good = dict(weight=A, dtype=0, vocab=5, dim=6, stride=6, ids=A, n=3, count=None, scale=1.0, out=A, out_stride=6, stream=None)
+    call("embed_tokens", good, [("weight", None), ("weight", A + 2), ("dtype", 7), ("vocab", 0), ("vocab", -1), ("dim", 0), ("dim", BIG),
+                                ("stride", 5), ("ids", None), ("ids", A + 1), ("n", -1), ("n", 1 << 30), ("count", A + 4), ("out", None),
+                                ("out", A + 2), ("out_stride", 5)])
+    assert _ops._load().bpe_embed_tokens(*{**good, "n": 0, "ids": None, "out": None}.values()) == 0
+    good = dict(grad=A, dtype=1, grad_stride=6, ids=A, n=3, count=None, vocab=5, dim=6, scale=1.0, accumulate=0, out=A, out_dtype=0,
+                out_stride=6, **WORK)
+    call("embed_tokens_grad", good, [("grad", None), ("grad", A + 1), ("dtype", 2 + 1), ("grad_stride", 5), ("ids", None), ("n", -1),
+                                     ("count", A + 1), ("vocab", 0), ("dim", 0), ("out", None), ("out", A + 2), ("out_dtype", 2),
+                                     ("out_dtype", 9), ("out_stride", 5), *BAD_WORK])
+
+
+def test_logits_arguments():
+    call("token_logprobs", dict(LOGITS, logprobs=A, lse=A, **WORK), [*BAD_LOGITS, ("logprobs", A + 2), ("lse", A + 1), *BAD_WORK])
+    call("token_logprobs_grad", dict(LOGITS, lse=A, upstream=A, grad=A, grad_stride=7, stream=None),
+         [*BAD_LOGITS, ("lse", None), ("upstream", None), ("upstream", A + 1), *BAD_GRAD])
+    call("token_logprobs_and_grad", dict(LOGITS, upstream=A, logprobs=A, lse=A, grad=A, grad_stride=7, **WORK),
+         [*BAD_LOGITS, ("upstream", None), ("logprobs", A + 1), ("lse", A + 1), *BAD_GRAD, *BAD_WORK])
+    call("next_tokens", dict(ids=A, n=3, offsets=A, batch=2, first=None, targets=A, stream=None),
+         [("ids", None), ("ids", A + 1), ("n", -1), ("offsets", None), ("offsets", A + 4), ("batch", -1), ("first", A + 1), ("targets", None)])
+
+
+def test_loss_arguments():
+    nan, inf = float("nan"), float("inf")
+    call("preference_loss", dict(LOGITS, offsets=A, batch=2, reference=None, beta=0.1, smoothing=0.0, scale=1.0, loss=A, margins=None,
+                                 logprobs=None, grad=A, grad_stride=7, **WORK),
+         [*BAD_LOGITS, ("offsets", None), ("offsets", A + 4), ("batch", -2), ("batch", 3), ("reference", A + 1), ("beta", nan), ("beta", inf),
+          ("smoothing", -0.1), ("smoothing", 1.1), ("smoothing", nan), ("scale", nan), ("loss", None), ("margins", A + 1), ("logprobs", A + 1),
+          *BAD_GRAD, *BAD_WORK])
+    call("policy_loss", dict(LOGITS, offsets=A, batch=2, old=A, advantages=A, advantage_by_string=0, reference=None, low=0.2, high=0.2, kl=0.0,
+                             by_string=0, scale=1.0, loss=A, logprobs=None, grad=A, grad_stride=7, **WORK),
+         [*BAD_LOGITS, ("offsets", None), ("batch", -1), ("old", None), ("advantages", None), ("reference", A + 1), ("low", -0.1), ("low", 1.1),
+          ("low", nan), ("high", -0.1), ("high", inf), ("kl", -1.0), ("kl", nan), ("scale", inf), ("loss", None), ("loss", A + 2), *BAD_GRAD,
+          *BAD_WORK])
+
+
+def test_workspaces():
+    lib = _ops._load()
+    for n, vocab, dim in ((-1, 5, 5), (5, 0, 5), (5, 5, 0), (1 << 30, 5, 5), (5, BIG, 5), (5, 5, BIG)):
+        assert lib.bpe_embed_tokens_grad_workspace_bytes(n, vocab, dim) == 0
+    for n, vocab, batch in ((-1, 5, 0), (5, 0, 0), (5, 5, -1), (1 << 30, 5, 0)):
+        assert lib.bpe_logits_workspace_bytes(n, vocab, batch) == 0
+    for n in (0, 1, 1000, 100000):
+        assert lib.bpe_embed_tokens_grad_workspace_bytes(n, 100260, 513) > 0
+        assert lib.bpe_logits_workspace_bytes(n, 100260, 0) > 0
+        assert lib.bpe_logits_workspace_bytes(n, 100260, 64) >= lib.bpe_logits_workspace_bytes(n, 100260, 0)
+
+
+def test_tensors_that_are_not_on_the_gpu_are_refused():
+    import pytest
+    import torch
+
+    ids, x = torch.zeros(3, dtype=torch.int32), torch.zeros(3, 5)
+    offsets = torch.tensor([0, 2, 3])
+    for bad in (lambda: bpe.embed_tokens(x, ids), lambda: bpe.embed_tokens_grad(x, ids, 4), lambda: bpe.next_tokens(ids, offsets),
+                lambda: bpe.token_logprobs(x, ids), lambda: bpe.token_logprobs_grad(x, ids, x[:, 0], x[:, 0]),
+                lambda: bpe.token_logprobs_and_grad(x, ids, x[:, 0]), lambda: bpe.preference_loss(x, ids, offsets),
+                lambda: bpe.policy_loss(x, ids, offsets, x[:, 0], x[:, 0])):
+        with pytest.raises(ValueError):
+            bad()
