@@ -1,5 +1,10 @@
 // Types of the matrices that the operators on token batches read and write: float, bfloat16, half.  Everything is computed in
 // 32 bits; a result is rounded once, to nearest even, where it is stored.
+//
+// Rows are read and written 16 bytes a lane from the row's first element on, whatever its address: rows of a vocabulary of
+// 100,260 tokens begin at every multiple of 8 bytes, and a view may begin at any element.  The hardware takes such addresses
+// in global memory; a row that is read from its own 16-byte boundaries instead needs a head, a tail and, where the gradient's
+// rows lie differently, a second way to write.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -16,5 +21,62 @@ template <typename T>
 __device__ inline T from_float(float x) { return (T)x; }
 
 constexpr float kLog2e = 1.44269504088896340736f;
+
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
+
+// 16 bytes of a row.
+template <typename T>
+struct Vec {
+  static constexpr int kWidth = 16 / sizeof(T);
+  Words w;
+
+  __device__ static Vec load(const T* p) {
+    struct __attribute__((packed, aligned(alignof(T)))) At { Words w; };
+    return {((const At*)p)->w};
+  }
+  __device__ void store(T* p) const {
+    struct __attribute__((packed, aligned(alignof(T)))) At { Words w; };
+    ((At*)p)->w = w;
+  }
+  __device__ void get(float (&x)[kWidth]) const {
+    if constexpr (sizeof(T) == 4) {
+      for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+    } else if constexpr (__is_same(T, bf16)) {
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    } else {
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = (float)__builtin_bit_cast(f16, (uint16_t)w[i]);
+        x[2 * i + 1] = (float)__builtin_bit_cast(f16, (uint16_t)(w[i] >> 16));
+      }
+    }
+  }
+  __device__ static Vec of(const float (&x)[kWidth]) {
+    Vec v;
+    if constexpr (sizeof(T) == 4) {
+      for (int i = 0; i < 4; ++i) v.w[i] = __float_as_uint(x[i]);
+    } else {
+      for (int i = 0; i < 4; ++i)
+        v.w[i] = (uint32_t)__builtin_bit_cast(uint16_t, (T)x[2 * i]) | (uint32_t)__builtin_bit_cast(uint16_t, (T)x[2 * i + 1]) << 16;
+    }
+    return v;
+  }
+  // Every element the same.
+  __device__ static Vec all(float x) {
+    float v[kWidth];
+    for (int i = 0; i < kWidth; ++i) v[i] = x;
+    return of(v);
+  }
+};
+
+// The larger of three.  (fmaxf first quiets each operand that the compiler cannot tell to be no signalling NaN, an instruction
+// more for each logit.)
+__device__ inline float max_of(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 }  // namespace bpe

@@ -15,20 +15,77 @@ __device__ inline float reference_of(float m) { return m == -INFINITY ? 0.0f : m
 // exp(x - r).  The difference first: a multiple of the type's lowest value would be -inf, and -inf minus itself NaN.
 __device__ inline float exp_of(float x, float r) { return __builtin_amdgcn_exp2f((x - r) * kLog2e); }
 
+// (Both sides the same whichever of them is whose: no product is fused with the addition.)
 __device__ inline Stats join(Stats a, Stats b) {
+#pragma clang fp contract(off)
   const float m = fmaxf(a.m, b.m), r = reference_of(m);
   return {m, a.s * exp_of(a.m, r) + b.s * exp_of(b.m, r)};
 }
 
+// Some more of a row's logits: one maximum and one change of reference for all of them.
+template <typename T, int kVecs>
+__device__ inline void absorb(Stats& stats, const Vec<T>* v) {
+  constexpr int kWidth = Vec<T>::kWidth;
+  float m = stats.m;
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    float x[kWidth];
+    v[k].get(x);
+#pragma unroll
+    for (int i = 0; i < kWidth; i += 2) m = max_of(m, x[i], x[i + 1]);
+  }
+  const float r = reference_of(m);
+  float s0 = stats.s * exp_of(stats.m, r), s1 = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    float x[kWidth];
+    v[k].get(x);
+#pragma unroll
+    for (int i = 0; i < kWidth; i += 2) {
+      s0 += exp_of(x[i], r);
+      s1 += exp_of(x[i + 1], r);
+    }
+  }
+  stats = {m, s0 + s1};
+}
+
+// The statistics of all threads' logits, in every thread, joined in a fixed order.
 template <int kThreads>
 __device__ inline Stats join_workgroup(Stats mine) {
-  __shared__ Stats part[kThreads / 64];
   for (int d = 32; d >= 1; d >>= 1) mine = join(mine, {__shfl_xor(mine.m, d), __shfl_xor(mine.s, d)});
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
-  __syncthreads();
-  Stats all = part[0];
-  for (int w = 1; w < kThreads / 64; ++w) all = join(all, part[w]);
-  return all;
+  if constexpr (kThreads > 64) {
+    __shared__ Stats part[kThreads / 64];
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    mine = part[threadIdx.x & (kThreads / 64 - 1)];
+    for (int d = kThreads / 128; d >= 1; d >>= 1) mine = join(mine, {__shfl_xor(mine.m, d), __shfl_xor(mine.s, d)});
+  }
+  return mine;
+}
+
+// The statistics of this thread's part of the elements [begin, end) of a row, 16 bytes a lane, four loads in flight.
+template <typename T, int kThreads>
+__device__ inline Stats stream(const T* x, int64_t begin, int64_t end) {
+  constexpr int kWidth = Vec<T>::kWidth, kDeep = 4;
+  Stats stats = {-INFINITY, 0.0f};
+  const T* at = x + begin + (int64_t)threadIdx.x * kWidth;
+  int64_t left = (end - begin) / kWidth;                    // whole vectors, and what is behind them
+  const int rest = (int)((end - begin) % kWidth);
+  for (; left >= kDeep * kThreads; left -= kDeep * kThreads, at += kDeep * kThreads * kWidth) {
+    Vec<T> v[kDeep];
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) v[k] = Vec<T>::load(at + k * kThreads * kWidth);
+    absorb<T, kDeep>(stats, v);
+  }
+  Vec<T> v[kDeep];
+#pragma unroll
+  for (int k = 0; k < kDeep; ++k) {
+    v[k] = Vec<T>::all(-INFINITY);
+    if (k * kThreads + (int)threadIdx.x < left) v[k] = Vec<T>::load(at + k * kThreads * kWidth);
+  }
+  absorb<T, kDeep>(stats, v);
+  if ((int)threadIdx.x < rest) stats = join(stats, {to_float(x[end - rest + (int)threadIdx.x]), 1.0f});
+  return stats;
 }
 
 // The logarithm of a token's probability, in 64 bits: x - m is exact or nearly so, and the logarithm's rounding to 32 bits
@@ -68,68 +125,225 @@ __device__ inline float policy_value(const RowArgs& a, int64_t t, double lp, flo
   return value;
 }
 
-// One workgroup a row: statistics, then what the row is for.
-template <typename T, int kKind>
-__global__ void __launch_bounds__(256) row_kernel(const T* logits, int64_t vocab, int64_t stride, RowArgs a, T* grad) {
-  const int64_t t = blockIdx.x;
-  const T* x = logits + t * stride;
-  T* g = grad + t * a.grad_stride;
-  const int32_t target = a.targets[t];
-  const float weight = kKind == kRowPolicy ? a.weight[t] : 1.0f;
-  const bool scored = target >= 0 && target < vocab && weight != 0.0f;
-  if (!scored) {
-    if (threadIdx.x == 0) {
-      if (a.logprobs) a.logprobs[t] = 0.0f;
-      if (a.lse) a.lse[t] = 0.0f;
-      if (a.logprobs64) a.logprobs64[t] = 0.0;
-      if (kKind == kRowPolicy) a.value[t] = 0.0;
-    }
-    if (kKind != kRowLogprob)
-      for (int64_t j = threadIdx.x; j < vocab; j += 256) g[j] = from_float<T>(0.0f);
-    return;
-  }
-  Stats mine = {-INFINITY, 0.0f};
-  for (int64_t j = threadIdx.x; j < vocab; j += 256) mine = join(mine, {to_float(x[j]), 1.0f});
-  const float at_target = to_float(x[target]);
-  const Stats all = join_workgroup<256>(mine);
-  const double lp = logprob_of(at_target, all);
+// What a row's log-probability gives besides: the outputs of thread 0, and the factor of the row's gradient.
+template <int kKind>
+__device__ inline float finish_row(const RowArgs& a, int64_t t, float weight, Stats all, double lp) {
   if (threadIdx.x == 0) {
     if (a.logprobs) a.logprobs[t] = (float)lp;
     if (a.lse) a.lse[t] = (float)((double)all.m + log((double)all.s));
     if (a.logprobs64) a.logprobs64[t] = lp;
   }
-  if (kKind == kRowLogprob) return;
-  float c = 0.0f;
-  if (kKind == kRowStep) c = a.upstream[t];
-  if (kKind == kRowPolicy) {
+  if constexpr (kKind == kRowStep) return a.upstream[t];
+  if constexpr (kKind == kRowPolicy) {
     float slope;
     const float value = policy_value(a, t, lp, &slope);
     if (threadIdx.x == 0) a.value[t] = (double)weight * value;
-    c = a.scale * weight * slope;
+    return a.scale * weight * slope;
   }
-  if (c == 0.0f) {
-    for (int64_t j = threadIdx.x; j < vocab; j += 256) g[j] = from_float<T>(0.0f);
-    return;
-  }
-  const float share = -c / all.s;
-  for (int64_t j = threadIdx.x; j < vocab; j += 256)
-    g[j] = from_float<T>(j == target ? -c * expm1f((float)lp) : share * exp_of(to_float(x[j]), all.m));
+  return 0.0f;
 }
 
+template <int kKind>
+__device__ inline void skip_row(const RowArgs& a, int64_t t) {
+  if (threadIdx.x == 0) {
+    if (a.logprobs) a.logprobs[t] = 0.0f;
+    if (a.lse) a.lse[t] = 0.0f;
+    if (a.logprobs64) a.logprobs64[t] = 0.0;
+    if (kKind == kRowPolicy) a.value[t] = 0.0;
+  }
+}
+
+template <int kKind>
+__device__ inline bool scored_row(const RowArgs& a, int64_t t, int64_t vocab, int32_t* target, float* weight) {
+  *target = a.targets[t];
+  *weight = kKind == kRowPolicy ? a.weight[t] : 1.0f;
+  return *target >= 0 && *target < vocab && *weight != 0.0f;
+}
+
+template <typename T, int kThreads>
+__device__ inline void zero_row(T* g, int64_t vocab) {
+  constexpr int kWidth = Vec<T>::kWidth;
+  const int64_t whole = vocab / kWidth;
+  for (int64_t j = threadIdx.x; j < whole; j += kThreads) Vec<T>::all(0.0f).store(g + j * kWidth);
+  const int64_t j = whole * kWidth + threadIdx.x;
+  if (j < vocab) g[j] = from_float<T>(0.0f);
+}
+
+// share x exp(x - reference) of the elements of a vector.
 template <typename T>
-__global__ void __launch_bounds__(256) logprobs_grad_kernel(const T* logits, int64_t vocab, int64_t stride,
+__device__ inline Vec<T> grad_of(const Vec<T>& v, float reference, float share) {
+  float x[Vec<T>::kWidth];
+  v.get(x);
+#pragma unroll
+  for (int i = 0; i < Vec<T>::kWidth; ++i) x[i] = share * exp_of(x[i], reference);
+  return Vec<T>::of(x);
+}
+
+// Log-probabilities alone, one workgroup a row.
+template <typename T>
+__global__ void __launch_bounds__(256) logprobs_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, RowArgs a) {
+  const int64_t t = first + blockIdx.x;
+  int32_t target;
+  float weight;
+  if (!scored_row<kRowLogprob>(a, t, vocab, &target, &weight)) return skip_row<kRowLogprob>(a, t);
+  const T* x = logits + t * stride;
+  const float at_target = to_float(x[target]);
+  const Stats all = join_workgroup<256>(stream<T, 256>(x, 0, vocab));
+  if (threadIdx.x == 0) finish_row<kRowLogprob>(a, t, weight, all, logprob_of(at_target, all));
+}
+
+// Few rows: each is split among `parts` workgroups, whose statistics another kernel joins.
+template <typename T>
+__global__ void __launch_bounds__(256) logprobs_part_kernel(const T* logits, int64_t vocab, int64_t stride, const int32_t* targets,
+                                                            unsigned parts, int64_t each, Stats* part) {
+  const int64_t t = blockIdx.x / parts, begin = blockIdx.x % parts * each, end = min(vocab, begin + each);
+  const int32_t target = targets[t];
+  if (target < 0 || target >= vocab) return;
+  const Stats all = join_workgroup<256>(stream<T, 256>(logits + t * stride, begin, end));
+  if (threadIdx.x == 0) part[blockIdx.x] = all;
+}
+
+// One wave a row.
+template <typename T>
+__global__ void __launch_bounds__(64) logprobs_join_kernel(const T* logits, int64_t vocab, int64_t stride, int parts,
+                                                           const Stats* part, RowArgs a) {
+  const int64_t t = blockIdx.x;
+  int32_t target;
+  float weight;
+  if (!scored_row<kRowLogprob>(a, t, vocab, &target, &weight)) return skip_row<kRowLogprob>(a, t);
+  const float at_target = to_float(logits[t * stride + target]);
+  Stats mine = {-INFINITY, 0.0f};
+  for (int k = threadIdx.x; k < parts; k += 64) mine = join(mine, part[t * parts + k]);
+  const Stats all = join_workgroup<64>(mine);
+  if (threadIdx.x == 0) finish_row<kRowLogprob>(a, t, weight, all, logprob_of(at_target, all));
+}
+
+// Log-probability and gradient of a row in one pass: the row stays in the workgroup's registers, kVecs x 16 bytes a lane.
+template <typename T, int kKind, int kThreads, int kVecs, int kWaves>
+__global__ void __launch_bounds__(kThreads, kWaves) row_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, RowArgs a, T* grad) {
+  constexpr int kWidth = Vec<T>::kWidth, kDeep = kVecs < 4 || (kVecs > 16 && sizeof(T) == 2) ? 2 : 4;
+  __shared__ float factor[2];
+  const int64_t t = first + blockIdx.x;
+  T* g = grad + t * a.grad_stride;
+  int32_t target;
+  float weight;
+  if (!scored_row<kKind>(a, t, vocab, &target, &weight)) {
+    skip_row<kKind>(a, t);
+    return zero_row<T, kThreads>(g, vocab);
+  }
+  const T* x = logits + t * stride;
+  const int whole = (int)(vocab / kWidth), rest = (int)(vocab % kWidth);
+  const int lane_at = (int)threadIdx.x;
+  Vec<T> v[kVecs];
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    v[k] = Vec<T>::all(-INFINITY);
+    if (k * kThreads + lane_at < whole) v[k] = Vec<T>::load(x + (k * kThreads + lane_at) * kWidth);
+  }
+  float last = -INFINITY;                                   // one of those behind the whole vectors
+  if (lane_at < rest) last = to_float(x[whole * kWidth + lane_at]);
+  const float at_target = to_float(x[target]);
+  Stats mine = {-INFINITY, 0.0f};
+#pragma unroll
+  for (int k = 0; k + kDeep <= kVecs; k += kDeep) absorb<T, kDeep>(mine, v + k);
+  if constexpr (kVecs % kDeep) absorb<T, kVecs % kDeep>(mine, v + kVecs / kDeep * kDeep);
+  const Stats all = join_workgroup<kThreads>(join(mine, {last, 1.0f}));
+  if (threadIdx.x < 64) {
+    const double lp = logprob_of(at_target, all);
+    const float c = finish_row<kKind>(a, t, weight, all, lp);
+    if (threadIdx.x == 0) {
+      factor[0] = c;
+      factor[1] = -c * expm1f((float)lp);                   // the gradient at the target: 1 - p without the cancellation
+    }
+  }
+  __syncthreads();
+  const float c = factor[0];
+  if (c == 0.0f) return zero_row<T, kThreads>(g, vocab);
+  const float share = -c / all.s;
+  // (The logits are converted once more: kept as 32-bit numbers they would take twice the registers.)
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) asm("" : "+v"(v[k].w));
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k)
+    if (k * kThreads + lane_at < whole) grad_of(v[k], all.m, share).store(g + (k * kThreads + lane_at) * kWidth);
+  if (lane_at < rest) g[whole * kWidth + lane_at] = from_float<T>(share * exp_of(last, all.m));
+  // The target's element once more, by the thread that has just written it.
+  if (lane_at == (target < whole * kWidth ? target / kWidth % kThreads : target - whole * kWidth))
+    g[target] = from_float<T>(factor[1]);
+}
+
+// The same for rows that no workgroup's registers hold: they are read twice.
+template <typename T, int kKind>
+__global__ void __launch_bounds__(1024) long_row_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, RowArgs a, T* grad) {
+  constexpr int kWidth = Vec<T>::kWidth, kThreads = 1024;
+  __shared__ float factor[2];
+  const int64_t t = first + blockIdx.x;
+  T* g = grad + t * a.grad_stride;
+  int32_t target;
+  float weight;
+  if (!scored_row<kKind>(a, t, vocab, &target, &weight)) {
+    skip_row<kKind>(a, t);
+    return zero_row<T, kThreads>(g, vocab);
+  }
+  const T* x = logits + t * stride;
+  const float at_target = to_float(x[target]);
+  const Stats all = join_workgroup<kThreads>(stream<T, kThreads>(x, 0, vocab));
+  if (threadIdx.x < 64) {
+    const double lp = logprob_of(at_target, all);
+    const float c = finish_row<kKind>(a, t, weight, all, lp);
+    if (threadIdx.x == 0) {
+      factor[0] = c;
+      factor[1] = -c * expm1f((float)lp);                   // the gradient at the target: 1 - p without the cancellation
+    }
+  }
+  __syncthreads();
+  const float c = factor[0];
+  if (c == 0.0f) return zero_row<T, kThreads>(g, vocab);
+  const float share = -c / all.s;
+  const int64_t whole = vocab / kWidth;
+  for (int64_t j = threadIdx.x; j < whole; j += kThreads) grad_of(Vec<T>::load(x + j * kWidth), all.m, share).store(g + j * kWidth);
+  const int64_t j = whole * kWidth + threadIdx.x;
+  if (j < vocab) g[j] = from_float<T>(share * exp_of(to_float(x[j]), all.m));
+  if (threadIdx.x == (target < whole * kWidth ? target / kWidth % kThreads : target - whole * kWidth))
+    g[target] = from_float<T>(factor[1]);
+}
+
+// The gradient from a saved lse.  A workgroup has up to 1,024 vectors of a row, one of its `parts`.
+template <typename T>
+__global__ void __launch_bounds__(256) logprobs_grad_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, unsigned parts,
                                                             const int32_t* targets, const float* lse, const float* upstream,
                                                             T* grad, int64_t grad_stride) {
-  const int64_t t = blockIdx.x;
-  const T* x = logits + t * stride;
-  T* g = grad + t * grad_stride;
+  constexpr int kWidth = Vec<T>::kWidth, kDeep = 4;
+  const int64_t t = first + blockIdx.x / parts, begin = (int64_t)(blockIdx.x % parts) * (256 * kDeep * kWidth);
   const int32_t target = targets[t];
-  const float c = target >= 0 && target < vocab ? upstream[t] : 0.0f, l = c != 0.0f ? lse[t] : 0.0f;
-  for (int64_t j = threadIdx.x; j < vocab; j += 256) {
-    float d = 0.0f;
-    if (c != 0.0f) d = j == target ? -c * expm1f(to_float(x[j]) - l) : -c * exp_of(to_float(x[j]), l);
-    g[j] = from_float<T>(d);
+  const float c = target >= 0 && target < vocab ? upstream[t] : 0.0f;
+  const T* x = logits + t * stride + begin;
+  T* g = grad + t * grad_stride + begin;
+  const int64_t left = vocab - begin;
+  const int whole = (int)min(left / kWidth, (int64_t)(256 * kDeep)), at = threadIdx.x;
+  const int j = whole * kWidth + at;                        // one of those behind the whole vectors
+  const bool has_last = whole < 256 * kDeep && j < left;
+  if (c == 0.0f) {
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k)
+      if (k * 256 + at < whole) Vec<T>::all(0.0f).store(g + (k * 256 + at) * kWidth);
+    if (has_last) g[j] = from_float<T>(0.0f);
+    return;
   }
+  const float l = lse[t];
+  Vec<T> v[kDeep];
+#pragma unroll
+  for (int k = 0; k < kDeep; ++k)
+    if (k * 256 + at < whole) v[k] = Vec<T>::load(x + (k * 256 + at) * kWidth);
+  const int64_t target_at = target - begin;
+  const bool here = target_at >= 0 && (target_at < whole * kWidth ? target_at / kWidth % 256 == at : has_last && target_at == j);
+  float at_target = 0.0f;
+  if (here) at_target = to_float(x[target_at]);
+  if (has_last) g[j] = from_float<T>(-c * exp_of(to_float(x[j]), l));
+#pragma unroll
+  for (int k = 0; k < kDeep; ++k)
+    if (k * 256 + at < whole) grad_of(v[k], l, -c).store(g + (k * 256 + at) * kWidth);
+  if (here) g[target_at] = from_float<T>(-c * expm1f(at_target - l));
 }
 
 // ---- over strings --------------------------------------------------------------------------------------------

@@ -52,11 +52,15 @@ size_t place(size_t& total, size_t bytes) {
 
 // The parts of the workspace of the functions on logits.
 struct LogitsWorkspace {
-  size_t logprobs, values, upstream, advantage, counts, total;
+  size_t parts, logprobs, values, upstream, advantage, counts, total;
 };
+
+// Statistics of parts of rows: fewer than this many, and one for each row.
+constexpr int64_t kParts = 1024;
 
 LogitsWorkspace logits_layout(int64_t n, int32_t batch) {
   LogitsWorkspace w{};
+  w.parts = place(w.total, (size_t)(n + kParts) * sizeof(Stats));
   w.logprobs = place(w.total, (size_t)n * 8);
   w.values = place(w.total, (size_t)std::max<int64_t>(n, batch) * 8);
   w.upstream = place(w.total, (size_t)n * 4);
@@ -65,11 +69,57 @@ LogitsWorkspace logits_layout(int64_t n, int32_t batch) {
   return w;
 }
 
+// Launches of up to `most` workgroups over n rows, `each` a row: f(first row, rows).
+template <typename F>
+void for_rows(int64_t n, int64_t each, F&& f) {
+  const int64_t rows = std::max<int64_t>(1, ((int64_t)1 << 21) / each);
+  for (int64_t first = 0; first < n; first += rows) f(first, std::min(rows, n - first));
+}
+
+template <typename T>
+void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, const RowArgs& a, Stats* part, hipStream_t stream) {
+  constexpr int64_t kStep = 256 * Vec<T>::kWidth;           // 4 KiB of a row
+  const int64_t steps = (vocab + kStep - 1) / kStep;
+  int64_t parts = n < kParts / 2 ? std::min(kParts / n, (steps + 1) / 2) : 1;
+  const int64_t each = (steps + parts - 1) / parts * kStep;
+  parts = (vocab + each - 1) / each;
+  if (parts == 1) {
+    for_rows(n, 1, [&](int64_t first, int64_t rows) {
+      hipLaunchKernelGGL(logprobs_kernel<T>, dim3((unsigned)rows), dim3(256), 0, stream, logits, vocab, stride, first, a);
+    });
+    return;
+  }
+  hipLaunchKernelGGL(logprobs_part_kernel<T>, dim3((unsigned)(n * parts)), dim3(256), 0, stream, logits, vocab, stride, a.targets,
+                     (unsigned)parts, each, part);
+  hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)n), dim3(64), 0, stream, logits, vocab, stride, (int)parts, part, a);
+}
+
+template <typename T, int kKind>
+void launch_rows(const T* logits, int64_t n, int64_t vocab, int64_t stride, const RowArgs& a, T* grad, hipStream_t stream) {
+  // The smallest variant whose registers hold a row: threads x vectors a lane.
+  const int64_t vecs = vocab / Vec<T>::kWidth;
+  for_rows(n, 1, [&](int64_t first, int64_t rows) {
+    const auto launch = [&](auto kernel, int threads) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, stream, logits, vocab, stride, first, a, grad);
+    };
+    if (vecs <= 256 * 2) launch(row_kernel<T, kKind, 256, 2, 4>, 256);
+    else if (vecs <= 256 * 8) launch(row_kernel<T, kKind, 256, 8, 4>, 256);
+    else if (vecs <= 256 * 16) launch(row_kernel<T, kKind, 256, 16, 4>, 256);
+    else if (vecs <= 512 * 16) launch(row_kernel<T, kKind, 512, 16, 4>, 512);
+    else if (vecs <= 512 * 25) launch(row_kernel<T, kKind, 512, 25, 4>, 512);
+    else if (vecs <= 1024 * 25) launch(row_kernel<T, kKind, 1024, 25, 4>, 1024);
+    else launch(long_row_kernel<T, kKind>, 1024);
+  });
+}
+
 template <typename T>
 void launch_grad(const T* logits, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets, const float* lse,
                  const float* upstream, T* grad, int64_t grad_stride, hipStream_t stream) {
-  hipLaunchKernelGGL(logprobs_grad_kernel<T>, dim3((unsigned)n), dim3(256), 0, stream, logits, vocab, stride, targets, lse,
-                     upstream, grad, grad_stride);
+  const int64_t parts = (vocab / Vec<T>::kWidth + 1023) / 1024 + (vocab / Vec<T>::kWidth % 1024 == 0 && vocab % Vec<T>::kWidth);
+  for_rows(n, parts, [&](int64_t first, int64_t rows) {
+    hipLaunchKernelGGL(logprobs_grad_kernel<T>, dim3((unsigned)(rows * parts)), dim3(256), 0, stream, logits, vocab, stride, first,
+                       (unsigned)parts, targets, lse, upstream, grad, grad_stride);
+  });
 }
 
 }  // namespace
@@ -144,8 +194,7 @@ int bpe_token_logprobs(const void* logits, int dtype, int64_t n, int64_t vocab, 
   a.lse = lse;
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    hipLaunchKernelGGL((row_kernel<T, kRowLogprob>), dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream, (const T*)logits,
-                       vocab, stride, a, (T*)nullptr);
+    launch_logprobs((const T*)logits, n, vocab, stride, a, (Stats*)((char*)workspace + logits_layout(n, 0).parts), (hipStream_t)stream);
   });
   return launched();
 }
@@ -179,8 +228,7 @@ int bpe_token_logprobs_and_grad(const void* logits, int dtype, int64_t n, int64_
   a.grad_stride = grad_stride;
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    hipLaunchKernelGGL((row_kernel<T, kRowStep>), dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream, (const T*)logits, vocab,
-                       stride, a, (T*)grad);
+    launch_rows<T, kRowStep>((const T*)logits, n, vocab, stride, a, (T*)grad, (hipStream_t)stream);
   });
   return launched();
 }
@@ -210,8 +258,7 @@ int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab,
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
     if (n > 0) {
-      hipLaunchKernelGGL((row_kernel<T, kRowLogprob>), dim3((unsigned)n), dim3(256), 0, stream, (const T*)logits, vocab, stride,
-                         a, (T*)nullptr);
+      launch_logprobs((const T*)logits, n, vocab, stride, a, (Stats*)(ws + w.parts), stream);
       hipLaunchKernelGGL(zero_kernel, dim3(blocks(n, 256)), dim3(256), 0, stream, upstream, n);
     }
     if (batch > 0)
@@ -259,8 +306,7 @@ int bpe_policy_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int
                        by_string, advantages, advantage_by_string, (float*)(ws + w.upstream), (float*)(ws + w.advantage));
     with_type(dtype, [&](auto type) {
       using T = decltype(type);
-      hipLaunchKernelGGL((row_kernel<T, kRowPolicy>), dim3((unsigned)n), dim3(256), 0, stream, (const T*)logits, vocab, stride, a,
-                         (T*)grad);
+      launch_rows<T, kRowPolicy>((const T*)logits, n, vocab, stride, a, (T*)grad, stream);
     });
   }
   hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(256), 0, stream, a.value, n, loss);
