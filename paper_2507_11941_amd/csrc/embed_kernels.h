@@ -1,6 +1,7 @@
 // Rows of an embedding, and their gradient.
 #pragma once
 #include "element.h"
+#include "sort_tokens.h"
 
 namespace bpe {
 
@@ -8,47 +9,254 @@ __device__ inline int64_t rows_in_use(int64_t n, const int64_t* count) {
   return count ? min(n, max(*count, (int64_t)0)) : n;
 }
 
-// One workgroup a row.
-template <typename T>
+// A lookup: a wave copies up to kVecs x 64 vectors of one row; a row takes `parts` waves.
+template <typename T, int kVecs>
 __global__ void __launch_bounds__(256) embed_kernel(const T* weight, int64_t vocab, int64_t dim, int64_t weight_stride,
-                                                    const int32_t* ids, int64_t n, const int64_t* count, float scale, T* out,
-                                                    int64_t out_stride) {
-  const int64_t t = blockIdx.x;
+                                                    const int32_t* ids, int64_t first, int64_t n, unsigned parts, const int64_t* count,
+                                                    float scale, T* out, int64_t out_stride) {
+  constexpr int kWidth = Vec<T>::kWidth;
+  const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  const int64_t t = first + wave / parts, begin = (int64_t)(wave % parts) * (kVecs * 64 * kWidth);
   if (t >= rows_in_use(n, count)) return;
   const int32_t id = ids[t];
   const bool kept = id >= 0 && id < vocab;
+  const int lane = threadIdx.x & 63;
+  const int whole = (int)min((dim - begin) / kWidth, (int64_t)(kVecs * 64));
+  const int64_t last = begin + whole * kWidth + lane;       // one of those behind the whole vectors
+  const bool has_last = whole < kVecs * 64 && last < dim;
   const T* from = weight + (kept ? id : 0) * weight_stride;
   T* to = out + t * out_stride;
-  for (int64_t c = threadIdx.x; c < dim; c += 256) to[c] = from_float<T>(kept ? scale * to_float(from[c]) : 0.0f);
+  Vec<T> v[kVecs];
+  if (!kept) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k)
+      if (k * 64 + lane < whole) Vec<T>::all(0.0f).store(to + begin + (k * 64 + lane) * kWidth);
+    if (has_last) to[last] = from_float<T>(0.0f);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k)
+    if (k * 64 + lane < whole) v[k] = Vec<T>::load(from + begin + (k * 64 + lane) * kWidth);
+  if (has_last) to[last] = from_float<T>(scale * to_float(from[last]));
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k)
+    if (k * 64 + lane < whole) {
+      float x[kWidth];
+      v[k].get(x);
+#pragma unroll
+      for (int i = 0; i < kWidth; ++i) x[i] *= scale;
+      Vec<T>::of(x).store(to + begin + (k * 64 + lane) * kWidth);
+    }
 }
 
-// One workgroup a row of the vocabulary: it looks through the ids and adds the rows that name it, in order.
-template <typename T, typename O>
-__global__ void __launch_bounds__(256) embed_grad_kernel(const T* grad, int64_t grad_stride, const int32_t* ids, int64_t n,
-                                                         const int64_t* count, int64_t dim, float scale, int accumulate,
-                                                         O* out, int64_t out_stride) {
-  __shared__ int32_t found[256];
-  const int64_t rows = rows_in_use(n, count);
-  const int32_t v = (int32_t)blockIdx.x;
-  O* to = out + (int64_t)v * out_stride;
-  for (int64_t c0 = 0; c0 < dim; c0 += 256) {
-    const int64_t c = c0 + threadIdx.x;
-    float sum = 0.0f;
-    bool any = false;
-    for (int64_t t0 = 0; t0 < rows; t0 += 256) {
-      const int64_t t = t0 + threadIdx.x;
-      __syncthreads();
-      found[threadIdx.x] = t < rows && ids[t] == v;
-      __syncthreads();
-      for (int i = 0; i < 256; ++i)
-        if (found[i]) {
-          any = true;
-          if (c < dim) sum += to_float(grad[(t0 + i) * grad_stride + c]);
-        }
+// ---- the gradient --------------------------------------------------------------------------------------------
+//
+// Positions come sorted by token, so that a token's rows are one run.  A wave has the runs of one chunk of up to 32 positions
+// in 64 x (16 bytes) of the columns: a run belongs to the chunk in which it begins and is summed by its wave alone, also where
+// it goes on into the next chunk, if it is no longer than a chunk.  A longer run is summed in pieces, one for each chunk that it
+// touches, in 32 bits in the workspace, and another kernel adds those.  Which rows are added in which order follows from the
+// sorted ids alone.
+
+constexpr int kChunk = 32;                                   // positions of a chunk at most: a wave's lanes hold it and the next
+
+struct GradArgs {
+  const uint32_t* keys;
+  const uint32_t* positions;
+  int64_t n;
+  uint32_t vocab;
+  int chunk;                                                 // positions of a chunk
+  int64_t chunks;
+  int64_t dim;
+  unsigned tiles;                                            // of the columns
+  int64_t grad_stride, out_stride;
+  float scale;
+  int accumulate;
+  float* pieces;                                             // [chunks][2][dim]: of a run from before, of one that goes on
+};
+
+// A lane's columns: kWidth of them from `load` on.  Where a row does not end with a whole vector its last vector begins earlier,
+// and the lane keeps only the columns from `own` on.  Rows narrower than a vector are one lane's, element by element.
+struct Columns {
+  int64_t load, own, end;
+};
+
+template <typename T>
+__device__ inline Columns columns_of(int64_t tile, int64_t dim) {
+  constexpr int kWidth = Vec<T>::kWidth;
+  const int64_t own = (tile * 64 + (threadIdx.x & 63)) * kWidth;
+  return {max((int64_t)0, min(own, dim - kWidth)), own, min(own + kWidth, dim)};
+}
+
+template <typename T>
+__device__ inline Vec<T> load_columns(const T* row, const Columns& c, int64_t dim) {
+  if (dim >= Vec<T>::kWidth) return Vec<T>::load(row + c.load);
+  float x[Vec<T>::kWidth] = {};
+  for (int i = 0; i < Vec<T>::kWidth; ++i)
+    if (i < dim) x[i] = to_float(row[i]);
+  return Vec<T>::of(x);
+}
+
+template <int kWidth, typename O>
+__device__ inline void store_columns(O* row, const Columns& c, const float (&sum)[kWidth], float scale, int accumulate) {
+  if (c.own >= c.end) return;
+  if (c.load == c.own && c.end - c.own == kWidth) {
+    float x[kWidth];
+#pragma unroll
+    for (int i = 0; i < kWidth; ++i) x[i] = scale * sum[i];
+    constexpr int kOut = Vec<O>::kWidth;
+#pragma unroll
+    for (int h = 0; h < kWidth / kOut; ++h) {
+      float y[kOut];
+      if (accumulate) Vec<O>::load(row + c.own + h * kOut).get(y);
+#pragma unroll
+      for (int i = 0; i < kOut; ++i) y[i] = accumulate ? y[i] + x[h * kOut + i] : x[h * kOut + i];
+      Vec<O>::of(y).store(row + c.own + h * kOut);
     }
-    if (c < dim && (any || !accumulate))
-      to[c] = from_float<O>(any ? (accumulate ? to_float(to[c]) : 0.0f) + scale * sum : 0.0f);
+    return;
   }
+#pragma unroll
+  for (int i = 0; i < kWidth; ++i) {
+    const int64_t col = c.load + i;
+    if (col >= c.own && col < c.end) row[col] = from_float<O>((accumulate ? to_float(row[col]) : 0.0f) + scale * sum[i]);
+  }
+}
+
+// The first place in the sorted keys that is not below `key`.
+__device__ inline int64_t lower_bound(const uint32_t* keys, int64_t n, uint32_t key) {
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (keys[mid] < key) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
+constexpr int kZeroRows = 16;                                // rows of the vocabulary that a wave looks for and clears
+
+// Waves below `summing` sum a chunk in a tile of the columns; the others clear rows that no id names.
+template <typename T, typename O>
+__global__ void __launch_bounds__(256) embed_grad_kernel(const T* grad, O* out, GradArgs a, int64_t first, int64_t summing) {
+  constexpr int kWidth = Vec<T>::kWidth, kDeep = 8;
+  const int64_t wave = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (wave >= summing) {
+    const int64_t v0 = (wave - summing) * kZeroRows;
+    if (a.accumulate || v0 >= a.vocab) return;
+    bool absent = false;
+    if (lane < kZeroRows && v0 + lane < a.vocab) {
+      const int64_t at = lower_bound(a.keys, a.n, (uint32_t)(v0 + lane));
+      absent = at >= a.n || a.keys[at] != (uint32_t)(v0 + lane);
+    }
+    uint64_t rows = __ballot(absent);
+    constexpr int kOut = Vec<O>::kWidth;
+    const int64_t whole = a.dim / kOut;
+    for (; rows; rows &= rows - 1) {
+      O* row = out + (v0 + __ffsll((unsigned long long)rows) - 1) * a.out_stride;
+      for (int64_t j = lane; j < whole; j += 64) Vec<O>::all(0.0f).store(row + j * kOut);
+      if (whole * kOut + lane < a.dim) row[whole * kOut + lane] = from_float<O>(0.0f);
+    }
+    return;
+  }
+  const int64_t c = wave / a.tiles, tile = wave % a.tiles, begin = c * a.chunk;
+  if (begin >= a.n) return;
+  const int size = (int)min((int64_t)a.chunk, a.n - begin);
+  // Lane i: the chunk's position i, up to the next chunk's last; and the position a chunk before it.
+  const int64_t mine = begin + lane;
+  const bool in_reach = mine < a.n && lane < 2 * a.chunk;
+  const uint32_t key = in_reach ? a.keys[mine] : 0xffffffffu;
+  const uint32_t position = in_reach ? a.positions[mine] : 0u;
+  const uint32_t earlier = lane < a.chunk && mine >= a.chunk ? a.keys[mine - a.chunk] : 0xffffffffu;
+  const uint32_t first_key = __builtin_amdgcn_readlane(key, 0);
+  if (first_key >= a.vocab) return;                          // nothing but padding from here on
+  const Columns cols = columns_of<T>(tile, a.dim);
+  float* head = a.pieces + 2 * c * a.dim;
+  float* tail = head + a.dim;
+  // What is ours: from `from` to `to` (numbers of lanes), the first `head_end` of it a piece of a run from before.
+  int from = 0, head_end = 0;
+  const uint64_t same = __ballot(key == first_key);
+  const int first_end = (int)__builtin_ctzll(~same | ((uint64_t)1 << 63));        // where the first run ends, in reach
+  if (begin > 0 && __builtin_amdgcn_readlane(earlier, a.chunk - 1) == first_key) {
+    // how many of the positions before belong to it, up to a chunk
+    const uint64_t back = __ballot(earlier == first_key) << (64 - a.chunk);
+    const int before = (int)__builtin_clzll(~back);
+    // It is long if its position number `chunk` exists: that many from its beginning, which may be before all we see.
+    if (before >= a.chunk || first_end > a.chunk - before) head_end = min(first_end, size);
+    from = min(first_end, size);
+  }
+  int to = size;                                             // where the last run that begins here ends
+  bool tail_piece = false;
+  const uint32_t last_key = __builtin_amdgcn_readlane(key, size - 1);
+  int tail_begin = size;
+  if (last_key < a.vocab && begin + size < a.n && __builtin_amdgcn_readlane(key, size) == last_key && from < size) {
+    const uint64_t run = __ballot(key == last_key);
+    tail_begin = (int)__builtin_ctzll(run);
+    const int end = tail_begin + (int)__builtin_ctzll(~(run >> tail_begin) | ((uint64_t)1 << 63));
+    if (end - tail_begin > a.chunk) tail_piece = true; else to = end;
+  }
+  if (head_end > 0) from = 0;
+  const int n_rows = min(to, (int)__builtin_ctzll(~__ballot(key < a.vocab) | ((uint64_t)1 << 63)));      // (padding is behind all tokens)
+  float sum[kWidth] = {};
+  for (int r0 = from; r0 < n_rows; r0 += kDeep) {
+    Vec<T> v[kDeep];
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) {
+      const int r = min(r0 + k, n_rows - 1);
+      v[k] = load_columns(grad + (int64_t)(uint32_t)__builtin_amdgcn_readlane(position, r) * a.grad_stride, cols, a.dim);
+    }
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) {
+      const int r = r0 + k;
+      if (r >= n_rows) break;
+      const uint32_t now = __builtin_amdgcn_readlane(key, r);
+      float x[kWidth];
+      v[k].get(x);
+#pragma unroll
+      for (int i = 0; i < kWidth; ++i) sum[i] += x[i];
+      const bool last = r + 1 == n_rows || __builtin_amdgcn_readlane(key, min(r + 1, 63)) != now;
+      if (!last) continue;
+      if (r < head_end || (tail_piece && r >= tail_begin))
+        store_columns(r < head_end ? head : tail, cols, sum, 1.0f, 0);
+      else
+        store_columns(out + (int64_t)now * a.out_stride, cols, sum, a.scale, a.accumulate);
+#pragma unroll
+      for (int i = 0; i < kWidth; ++i) sum[i] = 0.0f;
+    }
+  }
+}
+
+// Long runs: one workgroup for the run, if there is one, that begins in a chunk and has more positions than a chunk, and a tile
+// of the columns.  Its four waves add a quarter of the pieces each.
+template <typename T, typename O>
+__global__ void __launch_bounds__(256) embed_grad_join_kernel(O* out, GradArgs a, int64_t first) {
+  constexpr int kWidth = Vec<T>::kWidth;
+  const int64_t c = (first + blockIdx.x) / a.tiles, tile = (first + blockIdx.x) % a.tiles, begin = c * a.chunk, end = begin + a.chunk;
+  if (end >= a.n) return;                                    // (the last chunk's runs end with it)
+  const uint32_t key = a.keys[end - 1];
+  if (key >= a.vocab || a.keys[end] != key) return;
+  if (begin > 0 && a.keys[begin - 1] == key) return;         // it begins before
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t run = __ballot(lane < a.chunk && a.keys[begin + min(lane, a.chunk - 1)] == key);
+  const int64_t start = begin + (int64_t)__builtin_ctzll(run);
+  if (start + a.chunk >= a.n || a.keys[start + a.chunk] != key) return;
+  const int64_t stop = lower_bound(a.keys, a.n, key + 1);
+  const int64_t pieces = (stop - 1) / a.chunk - c + 1, each = (pieces + 3) / 4;
+  const Columns cols = columns_of<T>(tile, a.dim);
+  __shared__ float part[4][64][kWidth];
+  float sum[kWidth] = {};
+  if (cols.own < cols.end)
+    for (int64_t j = wave * each; j < min(pieces, (wave + 1) * each); ++j) {
+      const float* piece = a.pieces + (2 * (c + j) + (j == 0)) * a.dim;
+#pragma unroll
+      for (int i = 0; i < kWidth; ++i)
+        if (cols.load + i < a.dim) sum[i] += piece[cols.load + i];
+    }
+#pragma unroll
+  for (int i = 0; i < kWidth; ++i) part[wave][lane][i] = sum[i];
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int i = 0; i < kWidth; ++i) sum[i] = part[0][lane][i] + part[1][lane][i] + part[2][lane][i] + part[3][lane][i];
+  store_columns(out + (int64_t)key * a.out_stride, cols, sum, a.scale, a.accumulate);
 }
 
 }  // namespace bpe

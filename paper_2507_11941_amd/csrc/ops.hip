@@ -76,6 +76,92 @@ void for_rows(int64_t n, int64_t each, F&& f) {
   for (int64_t first = 0; first < n; first += rows) f(first, std::min(rows, n - first));
 }
 
+// Whether so few rows or waves that each should do little.
+constexpr int64_t kFewWaves = 2048;                         // two for each SIMD
+
+template <typename T>
+void launch_embed(const T* weight, int64_t vocab, int64_t dim, int64_t weight_stride, const int32_t* ids, int64_t n,
+                  const int64_t* count, float scale, T* out, int64_t out_stride, hipStream_t stream) {
+  const auto launch = [&](auto kernel, int vecs) {
+    const int64_t columns = (int64_t)vecs * 64 * Vec<T>::kWidth, parts = (dim + columns - 1) / columns;
+    for_rows(n, parts, [&](int64_t first, int64_t rows) {
+      hipLaunchKernelGGL(kernel, dim3(blocks(rows * parts, 4)), dim3(256), 0, stream, weight, vocab, dim, weight_stride, ids, first, n,
+                         (unsigned)parts, count, scale, out, out_stride);
+    });
+  };
+  if (n * ((dim + 256 * Vec<T>::kWidth - 1) / (256 * Vec<T>::kWidth)) >= kFewWaves) launch(embed_kernel<T, 4>, 4);
+  else launch(embed_kernel<T, 1>, 1);
+}
+
+// The workspace of the embedding's gradient: keys and positions as they are and as the pass before left them.
+struct EmbedWorkspace {
+  size_t keys[2], positions[2], counts, pieces, total;
+  int chunk;
+  int64_t chunks;
+};
+
+EmbedWorkspace embed_layout(int64_t n, int64_t dim) {
+  EmbedWorkspace w{};
+  // A chunk's rows are summed by one wave: fewer of them where there would be too few waves.
+  const int64_t tiles = (dim + 511) / 512;
+  w.chunk = kChunk;
+  while (w.chunk > 8 && (n + w.chunk - 1) / w.chunk * tiles < kFewWaves) w.chunk /= 2;
+  w.chunks = (n + w.chunk - 1) / w.chunk;
+  for (int i = 0; i < 2; ++i) {
+    w.keys[i] = place(w.total, (size_t)n * 4);
+    w.positions[i] = place(w.total, (size_t)n * 4);
+  }
+  w.counts = place(w.total, (size_t)kSortGrid * kDigits * 4);
+  w.pieces = place(w.total, (size_t)w.chunks * 2 * dim * 4);
+  return w;
+}
+
+// Positions by token, into keys[0] and positions[0] of the workspace.
+void sort_tokens(const TokenKeys& in, char* ws, const EmbedWorkspace& w, hipStream_t stream) {
+  int width = 1;
+  while (in.vocab >> width) ++width;                        // of the largest key, which is `vocab`
+  const int passes = (width + kDigitBits - 1) / kDigitBits, bits = (width + passes - 1) / passes;
+  uint32_t *keys[2], *positions[2];
+  for (int i = 0; i < 2; ++i) {
+    keys[i] = (uint32_t*)(ws + w.keys[i]);
+    positions[i] = (uint32_t*)(ws + w.positions[i]);
+  }
+  if (in.n <= 4 * kSortThreads) {
+    hipLaunchKernelGGL(sort_small_kernel<4>, dim3(1), dim3(kSortThreads), 0, stream, in, bits, passes, keys[0], positions[0]);
+    return;
+  }
+  if (in.n <= 8 * kSortThreads) {
+    hipLaunchKernelGGL(sort_small_kernel<8>, dim3(1), dim3(kSortThreads), 0, stream, in, bits, passes, keys[0], positions[0]);
+    return;
+  }
+  uint32_t* counts = (uint32_t*)(ws + w.counts);
+  const int64_t most = (in.n + kSortGrid - 1) / kSortGrid, each = (most + kSortTile - 1) / kSortTile * kSortTile;
+  const dim3 grid(blocks(in.n, each));
+  for (int p = 0; p < passes; ++p) {
+    const int to = (passes - 1 - p) & 1, from = to ^ 1;
+    const auto pass = [&](auto count, auto scatter) {
+      hipLaunchKernelGGL(count, grid, dim3(kSortThreads), 0, stream, in, keys[from], p * bits, 1 << bits, each, counts);
+      hipLaunchKernelGGL(scatter, grid, dim3(kSortThreads), 0, stream, in, keys[from], positions[from], p * bits, bits, each, counts,
+                         keys[to], positions[to]);
+    };
+    if (p == 0) pass(sort_count_kernel<true>, sort_scatter_kernel<true>);
+    else pass(sort_count_kernel<false>, sort_scatter_kernel<false>);
+  }
+}
+
+template <typename T, typename O>
+void launch_embed_grad(const T* grad, O* out, GradArgs a, hipStream_t stream) {
+  constexpr int64_t kMost = (int64_t)1 << 22;               // workgroups of a launch
+  a.tiles = (unsigned)((a.dim + 64 * Vec<T>::kWidth - 1) / (64 * Vec<T>::kWidth));
+  const int64_t summing = a.chunks * a.tiles, waves = summing + (a.accumulate ? 0 : (a.vocab + kZeroRows - 1) / kZeroRows);
+  for (int64_t first = 0; first < waves; first += 4 * kMost)
+    hipLaunchKernelGGL((embed_grad_kernel<T, O>), dim3(blocks(std::min(4 * kMost, waves - first), 4)), dim3(256), 0, stream, grad, out, a,
+                       first, summing);
+  if (a.chunks < 2) return;
+  for (int64_t first = 0; first < summing; first += kMost)
+    hipLaunchKernelGGL((embed_grad_join_kernel<T, O>), dim3((unsigned)std::min(kMost, summing - first)), dim3(256), 0, stream, out, a, first);
+}
+
 template <typename T>
 void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, const RowArgs& a, Stats* part, hipStream_t stream) {
   constexpr int64_t kStep = 256 * Vec<T>::kWidth;           // 4 KiB of a row
@@ -134,15 +220,14 @@ int bpe_embed_tokens(const void* weight, int dtype, int64_t vocab, int64_t dim, 
   if (n == 0) return BPE_OK;
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    hipLaunchKernelGGL(embed_kernel<T>, dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream, (const T*)weight, vocab, dim,
-                       weight_stride, ids, n, count, scale, (T*)out, out_stride);
+    launch_embed((const T*)weight, vocab, dim, weight_stride, ids, n, count, scale, (T*)out, out_stride, (hipStream_t)stream);
   });
   return launched();
 }
 
 size_t bpe_embed_tokens_grad_workspace_bytes(int64_t n, int64_t vocab, int64_t dim) {
   if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS || dim < 1 || dim > BPE_MAX_COLUMNS) return 0;
-  return 256;
+  return embed_layout(n, dim).total;
 }
 
 int bpe_embed_tokens_grad(const void* grad, int dtype, int64_t grad_stride, const int32_t* ids, int64_t n,
@@ -153,12 +238,27 @@ int bpe_embed_tokens_grad(const void* grad, int dtype, int64_t grad_stride, cons
       !fits(ids, n, 4) || !aligned(count, 8) ||
       !is_workspace(workspace, workspace_bytes, bpe_embed_tokens_grad_workspace_bytes(n, vocab, dim)))
     return BPE_EINVAL;
+  const EmbedWorkspace w = embed_layout(n, dim);
+  char* ws = (char*)workspace;
+  if (n > 0) sort_tokens({ids, n, count, (uint32_t)vocab}, ws, w, (hipStream_t)stream);
+  GradArgs a{};
+  a.keys = (const uint32_t*)(ws + w.keys[0]);
+  a.positions = (const uint32_t*)(ws + w.positions[0]);
+  a.n = n;
+  a.vocab = (uint32_t)vocab;
+  a.chunk = w.chunk;
+  a.chunks = w.chunks;
+  a.dim = dim;
+  a.grad_stride = grad_stride;
+  a.out_stride = out_stride;
+  a.scale = scale;
+  a.accumulate = accumulate;
+  a.pieces = (float*)(ws + w.pieces);
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
     const auto launch = [&](auto out_type) {
       using O = decltype(out_type);
-      hipLaunchKernelGGL((embed_grad_kernel<T, O>), dim3((unsigned)vocab), dim3(256), 0, (hipStream_t)stream, (const T*)grad,
-                         grad_stride, ids, n, count, dim, scale, accumulate, (O*)grad_weight, out_stride);
+      launch_embed_grad((const T*)grad, (O*)grad_weight, a, (hipStream_t)stream);
     };
     if (out_dtype == BPE_F32) launch(float{});
     else launch(type);
