@@ -10,14 +10,15 @@ import ctypes
 from ._binding import _check, load_library
 
 _TYPES = {}                                      # torch dtype -> the library's number of it
-_lib = None
+_lib = torch = None                              # (the package can be imported without torch)
 
 
 def _load():
-    global _lib
+    global _lib, torch
     if _lib is None:
-        import torch
+        import torch as module
 
+        torch = module
         lib = load_library()
         vp, i, i32, i64, f, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
         for name, args in {
@@ -66,25 +67,23 @@ def _vector(t, what, dev, dtype, count):
 
 def _enqueue(name, dev, stream, tensors, call):
     """call(stream handle), on the tensors' device; tensors that do not belong to `stream` are kept until it is done with them."""
-    import torch
-
     if dev.index != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return _enqueue(name, dev, stream, tensors, call)
-    current = torch.cuda.current_stream(dev)
     if stream is None:
-        stream = current
-    elif stream != current:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
-    _check(call(stream.cuda_stream), "bpe_" + name)
+        code = call(torch._C._cuda_getCurrentRawStream(dev.index))      # (without the 2 us of making a Stream of it)
+    else:
+        if stream != torch.cuda.current_stream(dev):
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+        code = call(stream.cuda_stream)
+    if code != 0:
+        _check(code, "bpe_" + name)
 
 
 def _strings(offsets, dev):
     """(pointer, number of strings) of a batch's offsets."""
-    import torch
-
     pointer, batch = _vector(offsets, "offsets", dev, torch.int64, None), offsets.numel() - 1
     if not 0 <= batch < 1 << 31:
         raise ValueError("offsets must have a beginning and an end for each string")
@@ -96,8 +95,6 @@ def _pointer(t):
 
 
 def _workspace(given, need, dev, what):
-    import torch
-
     if need == 0:
         raise ValueError(f"{what}: sizes out of range")
     if given is None:
@@ -108,8 +105,6 @@ def _workspace(given, need, dev, what):
 
 
 def _count(count, dev):
-    import torch
-
     if count is not None and (count.device != dev or count.dtype != torch.int64 or count.numel() != 1):
         raise ValueError(f"count must be one int64 on {dev}")
     return _pointer(count)
@@ -119,9 +114,7 @@ def embed_tokens(weight, ids, scale: float = 1.0, count=None, out=None, stream=N
     """``out[t] = scale * weight[ids[t]]``: rows of an embedding [vocab, dim] for int32 ids [n]; zeros for an id outside the
     vocabulary (padding).  ``count``: one int64 on the GPU, from which row on ids and out are left alone (``out_offsets[-1:]``
     of an encoded batch, whose ids need not all be in use)."""
-    import torch
-
-    lib = _load()
+    lib = _lib or _load()
     stride, dev = _matrix(weight, "weight"), weight.device
     n, dim = ids.numel(), weight.shape[1]
     ids_ptr = _vector(ids, "ids", dev, torch.int32, None)
@@ -140,9 +133,7 @@ def embed_tokens_grad(grad, ids, vocab: int, scale: float = 1.0, count=None, out
     """The gradient [vocab, dim] of an embedding's weights from that of its output [n, dim]: row v is ``scale`` times the sum
     of grad[t] over the t with ids[t] = v.  Its type is ``out``'s or ``dtype``: float32 or grad's (the default).  With
     ``accumulate`` it is added to what ``out`` holds."""
-    import torch
-
-    lib = _load()
+    lib = _lib or _load()
     stride, dev = _matrix(grad, "grad"), grad.device
     n, dim = grad.shape
     ids_ptr = _vector(ids, "ids", dev, torch.int32, n)
@@ -166,9 +157,7 @@ def embed_tokens_grad(grad, ids, vocab: int, scale: float = 1.0, count=None, out
 def next_tokens(ids, offsets, first=None, out=None, stream=None):
     """What each position of a packed batch is to predict: the id after it in its string (int64 offsets [B + 1]); -1, not
     scored, at a string's end and where that id is among the string's ``first`` tokens (int32 [B]: prompts)."""
-    import torch
-
-    lib = _load()
+    lib = _lib or _load()
     dev, n = ids.device, ids.numel()
     if not ids.is_cuda:
         raise ValueError("ids must be on the GPU")
@@ -184,8 +173,6 @@ def next_tokens(ids, offsets, first=None, out=None, stream=None):
 
 
 def _grad_of(logits, out):
-    import torch
-
     if out is None:
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     stride = _matrix(out, "out", logits.device, tuple(logits.shape), logits.dtype)
@@ -199,9 +186,7 @@ def _logits_workspace(workspace, n, vocab, batch, dev):
 def token_logprobs(logits, targets, workspace=None, stream=None):
     """(log-probabilities float32 [n] of the int32 targets [n] under logits [n, vocab], logarithms float32 [n] of the rows'
     sums of exponentials).  Rows whose target is outside the vocabulary are not scored: not read, and 0 in both."""
-    import torch
-
-    lib = _load()
+    lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
     targets_ptr = _vector(targets, "targets", dev, torch.int32, n)
@@ -216,9 +201,7 @@ def token_logprobs(logits, targets, workspace=None, stream=None):
 def token_logprobs_grad(logits, targets, lse, upstream, out=None, stream=None):
     """The gradient [n, vocab] with respect to the logits of ``(upstream * logprobs).sum()``, from the ``lse`` that
     ``token_logprobs`` returned.  ``out`` may be ``logits`` itself."""
-    import torch
-
-    lib = _load()
+    lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
     targets_ptr = _vector(targets, "targets", dev, torch.int32, n)
@@ -233,9 +216,7 @@ def token_logprobs_grad(logits, targets, lse, upstream, out=None, stream=None):
 def token_logprobs_and_grad(logits, targets, upstream, out=None, workspace=None, stream=None):
     """(logprobs, lse, gradient of ``(upstream * logprobs).sum()``) in one pass over the logits, for an upstream that is known
     before: of cross entropy it is -1 / (number of scored tokens).  ``out`` may be ``logits`` itself."""
-    import torch
-
-    lib = _load()
+    lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
     targets_ptr = _vector(targets, "targets", dev, torch.int32, n)
@@ -255,9 +236,7 @@ def preference_loss(logits, targets, offsets, reference=None, beta: float = 0.1,
     """Preference loss over pairs of strings, 2k preferred to 2k + 1: (loss, margins float32 [B / 2], logprobs float32 [n],
     ``scale`` times the gradient with respect to the logits).  ``reference``: float32 [n], the reference model's logprobs.
     ``out`` may be ``logits`` itself.  The formulas are in include/bpe_ops.h."""
-    import torch
-
-    lib = _load()
+    lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
     targets_ptr = _vector(targets, "targets", dev, torch.int32, n)
@@ -284,9 +263,7 @@ def policy_loss(logits, targets, offsets, old, advantages, reference=None, clip_
     [n], or [B], one for all of a string (where n = B, it is by string if ``per`` is "string").  ``per``: "token", all scored
     tokens weigh the same, or "string", all strings.  ``out`` may be ``logits`` itself.  The formulas are in
     include/bpe_ops.h."""
-    import torch
-
-    lib = _load()
+    lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
     targets_ptr = _vector(targets, "targets", dev, torch.int32, n)

@@ -71,6 +71,7 @@ struct GradArgs {
   int64_t grad_stride, out_stride;
   float scale;
   int accumulate;
+  const uint8_t* present;                                    // whether there is a token; not used where it is accumulated
   float* pieces;                                             // [chunks][2][dim]: of a run from before, of one that goes on
 };
 
@@ -121,16 +122,6 @@ __device__ inline void store_columns(O* row, const Columns& c, const float (&sum
   }
 }
 
-// The first place in the sorted keys that is not below `key`.
-__device__ inline int64_t lower_bound(const uint32_t* keys, int64_t n, uint32_t key) {
-  int64_t lo = 0, hi = n;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (keys[mid] < key) lo = mid + 1; else hi = mid;
-  }
-  return lo;
-}
-
 constexpr int kZeroRows = 16;                                // rows of the vocabulary that a wave looks for and clears
 
 // Waves below `summing` sum a chunk in a tile of the columns; the others clear rows that no id names.
@@ -142,12 +133,7 @@ __global__ void __launch_bounds__(256) embed_grad_kernel(const T* grad, O* out, 
   if (wave >= summing) {
     const int64_t v0 = (wave - summing) * kZeroRows;
     if (a.accumulate || v0 >= a.vocab) return;
-    bool absent = false;
-    if (lane < kZeroRows && v0 + lane < a.vocab) {
-      const int64_t at = lower_bound(a.keys, a.n, (uint32_t)(v0 + lane));
-      absent = at >= a.n || a.keys[at] != (uint32_t)(v0 + lane);
-    }
-    uint64_t rows = __ballot(absent);
+    uint64_t rows = __ballot(lane < kZeroRows && v0 + lane < a.vocab && (a.n == 0 || !a.present[v0 + lane]));
     constexpr int kOut = Vec<O>::kWidth;
     const int64_t whole = a.dim / kOut;
     for (; rows; rows &= rows - 1) {
@@ -238,18 +224,35 @@ __global__ void __launch_bounds__(256) embed_grad_join_kernel(O* out, GradArgs a
   const uint64_t run = __ballot(lane < a.chunk && a.keys[begin + min(lane, a.chunk - 1)] == key);
   const int64_t start = begin + (int64_t)__builtin_ctzll(run);
   if (start + a.chunk >= a.n || a.keys[start + a.chunk] != key) return;
-  const int64_t stop = lower_bound(a.keys, a.n, key + 1);
-  const int64_t pieces = (stop - 1) / a.chunk - c + 1, each = (pieces + 3) / 4;
+  // The chunks that it goes on into begin with it.
+  int64_t pieces = 1;
+  for (;;) {
+    const int64_t at = (c + pieces + lane) * a.chunk;
+    const uint64_t more = __ballot(at < a.n && a.keys[min(at, a.n - 1)] == key);
+    pieces += more == ~(uint64_t)0 ? 64 : (int)__builtin_ctzll(~more);
+    if (more != ~(uint64_t)0) break;
+  }
+  const int64_t each = (pieces + 3) / 4, last = min(pieces, (wave + 1) * each);
   const Columns cols = columns_of<T>(tile, a.dim);
   __shared__ float part[4][64][kWidth];
   float sum[kWidth] = {};
-  if (cols.own < cols.end)
-    for (int64_t j = wave * each; j < min(pieces, (wave + 1) * each); ++j) {
-      const float* piece = a.pieces + (2 * (c + j) + (j == 0)) * a.dim;
+  if (a.dim >= kWidth) {
+#pragma unroll 4
+    for (int64_t j = wave * each; j < last; ++j) {
+      const float* piece = a.pieces + (2 * (c + j) + (j == 0)) * a.dim + cols.load;
 #pragma unroll
-      for (int i = 0; i < kWidth; ++i)
-        if (cols.load + i < a.dim) sum[i] += piece[cols.load + i];
+      for (int h = 0; h < kWidth; h += 4) {
+        float x[4];
+        Vec<float>::load(piece + h).get(x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[h + i] += x[i];
+      }
     }
+  } else if (cols.own < cols.end) {
+    for (int64_t j = wave * each; j < last; ++j)
+      for (int i = 0; i < kWidth; ++i)
+        if (i < a.dim) sum[i] += a.pieces[(2 * (c + j) + (j == 0)) * a.dim + i];
+  }
 #pragma unroll
   for (int i = 0; i < kWidth; ++i) part[wave][lane][i] = sum[i];
   __syncthreads();

@@ -102,7 +102,9 @@ struct RowArgs {
   const float* upstream;      // kRowStep
   int64_t grad_stride;
   // kRowPolicy
-  const float* weight;        // of each row's loss; 0: not in a string
+  const float* weight;        // of each row's loss; 0: not scored
+  const int32_t* scored;      // null, or the numbers of scored rows whose sum the loss is divided by
+  int n_scored;
   const float* advantage;     // of each row
   const float* old;
   const float* reference;
@@ -157,7 +159,14 @@ template <int kKind>
 __device__ inline bool scored_row(const RowArgs& a, int64_t t, int64_t vocab, int32_t* target, float* weight) {
   *target = a.targets[t];
   *weight = kKind == kRowPolicy ? a.weight[t] : 1.0f;
-  return *target >= 0 && *target < vocab && *weight != 0.0f;
+  const bool scored = *target >= 0 && *target < vocab && *weight != 0.0f;
+  if (kKind == kRowPolicy && scored && a.scored) {
+    int32_t all = 0;
+    for (int i = threadIdx.x & 63; i < a.n_scored; i += 64) all += a.scored[i];
+    for (int d = 32; d >= 1; d >>= 1) all += __shfl_xor(all, d);
+    *weight = 1.0f / (float)__builtin_amdgcn_readfirstlane(all);
+  }
+  return scored;
 }
 
 template <typename T, int kThreads>
@@ -180,15 +189,15 @@ __device__ inline Vec<T> grad_of(const Vec<T>& v, float reference, float share) 
 }
 
 // Log-probabilities alone, one workgroup a row.
-template <typename T>
-__global__ void __launch_bounds__(256) logprobs_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, RowArgs a) {
+template <typename T, int kThreads>
+__global__ void __launch_bounds__(kThreads) logprobs_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, RowArgs a) {
   const int64_t t = first + blockIdx.x;
   int32_t target;
   float weight;
   if (!scored_row<kRowLogprob>(a, t, vocab, &target, &weight)) return skip_row<kRowLogprob>(a, t);
   const T* x = logits + t * stride;
   const float at_target = to_float(x[target]);
-  const Stats all = join_workgroup<256>(stream<T, 256>(x, 0, vocab));
+  const Stats all = join_workgroup<kThreads>(stream<T, kThreads>(x, 0, vocab));
   if (threadIdx.x == 0) finish_row<kRowLogprob>(a, t, weight, all, logprob_of(at_target, all));
 }
 
@@ -308,11 +317,38 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const T* logits, int64_t
     g[target] = from_float<T>(factor[1]);
 }
 
+// The sum over a workgroup, in every thread, in a fixed order.
+template <int kThreads, typename V>
+__device__ inline V sum_workgroup(V mine) {
+  __shared__ V part[kThreads / 64];
+  for (int d = 32; d >= 1; d >>= 1) mine += __shfl_xor(mine, d);
+  __syncthreads();                                          // (the last sum's parts are read)
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  V all = part[0];
+#pragma unroll
+  for (int w = 1; w < kThreads / 64; ++w) all += part[w];
+  return all;
+}
+
+// The sum of values, by one workgroup.
+template <int kThreads>
+__device__ inline void sum_values(const double* values, int64_t n, float* sum) {
+  double mine = 0.0;
+#pragma unroll 8
+  for (int64_t i = threadIdx.x; i < n; i += kThreads) mine += values[i];
+  mine = sum_workgroup<kThreads>(mine);
+  if (threadIdx.x == 0) *sum = (float)mine;
+}
+
 // The gradient from a saved lse.  A workgroup has up to 1,024 vectors of a row, one of its `parts`.
+// With `loss`, one workgroup more: the loss is the sum of the pairs' losses.
 template <typename T>
 __global__ void __launch_bounds__(256) logprobs_grad_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, unsigned parts,
                                                             const int32_t* targets, const float* lse, const float* upstream,
-                                                            T* grad, int64_t grad_stride) {
+                                                            T* grad, int64_t grad_stride, const double* losses, int32_t n_losses,
+                                                            float* loss) {
+  if (blockIdx.x == gridDim.x - 1 && loss) return sum_values<256>(losses, n_losses, loss);
   constexpr int kWidth = Vec<T>::kWidth, kDeep = 4;
   const int64_t t = first + blockIdx.x / parts, begin = (int64_t)(blockIdx.x % parts) * (256 * kDeep * kWidth);
   const int32_t target = targets[t];
@@ -354,56 +390,66 @@ __device__ inline void string_rows(const int64_t* offsets, int32_t i, int64_t n,
   *end = max(*begin, min(offsets[i + 1], n));
 }
 
-__device__ inline int32_t string_of(const int64_t* offsets, int32_t batch, int64_t t) {
-  int32_t lo = 0, hi = batch;                              // the last string that begins at or before t
-  while (lo < hi) {
-    const int32_t mid = (lo + hi) >> 1;
-    if (offsets[mid + 1] <= t) lo = mid + 1; else hi = mid;
+// The string of row t, -1 outside; t is the lane's number further than the wave's first row.  All lanes take part: 64 offsets
+// are looked at together, so that up to 64 strings take one read, up to 4,096 two.  Lanes whose rows are in a later string than
+// the first lane's look for it on their own.
+__device__ inline int32_t string_of(const int64_t* offsets, int32_t batch, int64_t t, int lane) {
+  const int64_t first = t - lane;
+  int64_t lo = 0, hi = batch;                               // the first string that ends behind the wave's first row
+  while (hi - lo > 0) {
+    const int64_t step = (hi - lo + 63) / 64, at = lo + (lane + 1) * step - 1;
+    const uint64_t ends_before = __ballot(at < hi && offsets[min(at, hi - 1) + 1] <= first);
+    lo += (int64_t)__popcll(ends_before) * step;
+    hi = min(hi, lo + step - 1);
   }
-  return lo < batch && offsets[lo] <= t ? lo : -1;
+  if (lo < batch && offsets[lo + 1] <= t) {
+    ++lo;
+    hi = batch;
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) >> 1;
+      if (offsets[mid + 1] <= t) lo = mid + 1; else hi = mid;
+    }
+  }
+  return lo < batch && offsets[lo] <= t ? (int32_t)lo : -1;
 }
 
 __global__ void __launch_bounds__(256) next_tokens_kernel(const int32_t* ids, int64_t n, const int64_t* offsets, int32_t batch,
                                                           const int32_t* first, int32_t* targets) {
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int32_t i = string_of(offsets, batch, t, threadIdx.x & 63);
   if (t >= n) return;
-  const int32_t i = string_of(offsets, batch, t);
   const bool scored = i >= 0 && t + 1 < n && t + 1 < offsets[i + 1] && (!first || t + 1 - offsets[i] >= first[i]);
   targets[t] = scored ? ids[t + 1] : -1;
-}
-
-template <typename V>
-__device__ inline V sum_workgroup(V mine) {                 // of 256 threads, in a fixed order
-  __shared__ V part[256];
-  __syncthreads();
-  part[threadIdx.x] = mine;
-  __syncthreads();
-  for (int d = 128; d >= 1; d >>= 1) {
-    if ((int)threadIdx.x < d) part[threadIdx.x] += part[threadIdx.x + d];
-    __syncthreads();
-  }
-  return part[0];
 }
 
 __device__ inline bool is_scored(const int32_t* targets, int64_t t, int64_t vocab) {
   return targets[t] >= 0 && targets[t] < vocab;
 }
 
-// One workgroup a pair; `upstream` is zero before.
+// f(t) for the rows that are in no string.
+template <int kThreads, typename F>
+__device__ inline void rows_outside(const int64_t* offsets, int32_t batch, int64_t n, F&& f) {
+  const int64_t begin = batch > 0 ? min(max(offsets[0], (int64_t)0), n) : n, end = batch > 0 ? min(offsets[batch], n) : n;
+  for (int64_t t = threadIdx.x; t < begin; t += kThreads) f(t);
+  for (int64_t t = max(begin, end) + threadIdx.x; t < n; t += kThreads) f(t);
+}
+
+// One workgroup a pair: both sides' sums, the loss, and the factor of each row's gradient.  One more: rows outside every string.
 __global__ void __launch_bounds__(256) pair_kernel(const double* logprobs, const int32_t* targets, int64_t n, int64_t vocab,
                                                    const int64_t* offsets, int32_t batch, const float* reference, float beta,
                                                    float smoothing, float scale, float* margins, double* losses, float* upstream) {
   const int32_t k = blockIdx.x;
-  double sums[2];
-  for (int side = 0; side < 2; ++side) {
-    int64_t b, e;
-    string_rows(offsets, 2 * k + side, n, &b, &e);
-    double sum = 0.0;
-    for (int64_t t = b + threadIdx.x; t < e; t += 256)
-      if (is_scored(targets, t, vocab)) sum += logprobs[t] - (reference ? (double)reference[t] : 0.0);
-    sums[side] = sum_workgroup(sum);
-  }
-  const double z = (double)beta * (sums[0] - sums[1]);
+  if (k == batch / 2) return rows_outside<256>(offsets, batch, n, [&](int64_t t) { upstream[t] = 0.0f; });
+  int64_t begin, middle, end, unused;
+  string_rows(offsets, 2 * k, n, &begin, &middle);
+  string_rows(offsets, 2 * k + 1, n, &unused, &end);
+  double sum = 0.0;
+  for (int64_t t = begin + threadIdx.x; t < end; t += 256)
+    if (is_scored(targets, t, vocab)) {
+      const double apart = logprobs[t] - (reference ? (double)reference[t] : 0.0);
+      sum += t < middle ? apart : -apart;
+    }
+  const double z = (double)beta * sum_workgroup<256>(sum);
   // -log sigmoid(z) = max(-z, 0) + log(1 + exp(-|z|))
   const double tail = log1p(exp(-fabs(z)));
   const double loss = (1.0 - (double)smoothing) * (fmax(-z, 0.0) + tail) + (double)smoothing * (fmax(z, 0.0) + tail);
@@ -413,55 +459,57 @@ __global__ void __launch_bounds__(256) pair_kernel(const double* logprobs, const
     losses[k] = loss / (batch / 2);
     if (margins) margins[k] = (float)z;
   }
-  for (int side = 0; side < 2; ++side) {
-    int64_t b, e;
-    string_rows(offsets, 2 * k + side, n, &b, &e);
-    for (int64_t t = b + threadIdx.x; t < e; t += 256) upstream[t] = side ? -c : c;
+  for (int64_t t = begin + threadIdx.x; t < end; t += 256) upstream[t] = t < middle ? c : -c;
+}
+
+__global__ void __launch_bounds__(1024) sum_kernel(const double* values, int64_t n, float* sum) {
+  sum_values<1024>(values, n, sum);
+}
+
+constexpr int kWeightWaves = 16;                             // strings of a workgroup
+constexpr int kShortString = 4096;                           // positions that one wave goes over
+
+// The weight of each scored position in its string's loss and its advantage; and the number of scored positions of this
+// workgroup's strings.  A wave has a string, the whole workgroup one after the other those that are long.  The last workgroup:
+// rows outside every string.
+__global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(const int32_t* targets, int64_t n, int64_t vocab,
+                                                                    const int64_t* offsets, int32_t batch, int by_string,
+                                                                    const float* advantages, int advantage_by_string, float* weight,
+                                                                    float* advantage, int32_t* scored) {
+  constexpr int kThreads = 64 * kWeightWaves;
+  if (blockIdx.x == gridDim.x - 1) return rows_outside<kThreads>(offsets, batch, n, [&](int64_t t) { weight[t] = 0.0f; });
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  int32_t all = 0;                                           // of the waves' strings, in lane 0 of each; of long ones in thread 0
+  const auto fill = [&](int32_t i, int64_t begin, int64_t end, int at, int step, auto&& total) {
+    int32_t count = 0;
+#pragma unroll 4
+    for (int64_t t = begin + at; t < end; t += step) count += is_scored(targets, t, vocab);
+    count = total(count);
+    const float w = by_string ? (float)(1.0 / ((double)batch * max(count, 1))) : 1.0f;
+#pragma unroll 4
+    for (int64_t t = begin + at; t < end; t += step) {
+      const bool is = is_scored(targets, t, vocab);
+      weight[t] = is ? w : 0.0f;
+      if (is) advantage[t] = advantages[advantage_by_string ? i : t];
+    }
+    if (at == 0) all += count;
+  };
+  for (int32_t i0 = blockIdx.x * kWeightWaves; i0 < batch; i0 += (gridDim.x - 1) * kWeightWaves) {
+    const int32_t i = i0 + wave;
+    int64_t begin = 0, end = 0;
+    if (i < batch) string_rows(offsets, i, n, &begin, &end);
+    if (end - begin <= kShortString)
+      fill(i, begin, end, lane, 64, [](int32_t c) {
+        for (int d = 32; d >= 1; d >>= 1) c += __shfl_xor(c, d);
+        return c;
+      });
+    for (int32_t j = i0; j < min(i0 + kWeightWaves, batch); ++j) {
+      string_rows(offsets, j, n, &begin, &end);
+      if (end - begin > kShortString) fill(j, begin, end, threadIdx.x, kThreads, [](int32_t c) { return sum_workgroup<kThreads>(c); });
+    }
   }
-}
-
-__global__ void __launch_bounds__(256) sum_kernel(const double* values, int64_t n, float* sum) {
-  double mine = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 256) mine += values[i];
-  mine = sum_workgroup(mine);
-  if (threadIdx.x == 0) *sum = (float)mine;
-}
-
-__global__ void __launch_bounds__(256) zero_kernel(float* values, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) values[i] = 0.0f;
-}
-
-// One workgroup: how many positions of each string are scored, and of all together (in counts[batch]).
-__global__ void __launch_bounds__(256) count_kernel(const int32_t* targets, int64_t n, int64_t vocab, const int64_t* offsets,
-                                                    int32_t batch, int32_t* counts) {
-  int32_t all = 0;
-  for (int32_t i = 0; i < batch; ++i) {
-    int64_t b, e;
-    string_rows(offsets, i, n, &b, &e);
-    int32_t mine = 0;
-    for (int64_t t = b + threadIdx.x; t < e; t += 256) mine += is_scored(targets, t, vocab);
-    mine = sum_workgroup(mine);
-    if (threadIdx.x == 0) counts[i] = mine;
-    all += mine;
-  }
-  if (threadIdx.x == 0) counts[batch] = all;
-}
-
-__global__ void __launch_bounds__(256) weights_kernel(const int32_t* targets, int64_t n, int64_t vocab, const int64_t* offsets,
-                                                      int32_t batch, const int32_t* counts, int by_string,
-                                                      const float* advantages, int advantage_by_string, float* weight,
-                                                      float* advantage) {
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t >= n) return;
-  const int32_t i = string_of(offsets, batch, t);
-  float w = 0.0f, a = 0.0f;
-  if (i >= 0 && is_scored(targets, t, vocab)) {
-    w = by_string ? (float)(1.0 / ((double)batch * counts[i])) : (float)(1.0 / counts[batch]);
-    a = advantages[advantage_by_string ? i : t];
-  }
-  weight[t] = w;
-  advantage[t] = a;
+  all = sum_workgroup<kThreads>(lane == 0 ? all : 0);
+  if (threadIdx.x == 0) scored[blockIdx.x] = all;
 }
 
 }  // namespace bpe

@@ -55,6 +55,8 @@ struct LogitsWorkspace {
   size_t parts, logprobs, values, upstream, advantage, counts, total;
 };
 
+constexpr unsigned kWeightGroups = 256;                     // workgroups that count scored positions
+
 // Statistics of parts of rows: fewer than this many, and one for each row.
 constexpr int64_t kParts = 1024;
 
@@ -65,7 +67,7 @@ LogitsWorkspace logits_layout(int64_t n, int32_t batch) {
   w.values = place(w.total, (size_t)std::max<int64_t>(n, batch) * 8);
   w.upstream = place(w.total, (size_t)n * 4);
   w.advantage = place(w.total, (size_t)n * 4);
-  w.counts = place(w.total, ((size_t)batch + 1) * 4);
+  w.counts = place(w.total, kWeightGroups * 4);
   return w;
 }
 
@@ -95,12 +97,12 @@ void launch_embed(const T* weight, int64_t vocab, int64_t dim, int64_t weight_st
 
 // The workspace of the embedding's gradient: keys and positions as they are and as the pass before left them.
 struct EmbedWorkspace {
-  size_t keys[2], positions[2], counts, pieces, total;
+  size_t keys[2], positions[2], counts, present, pieces, total;
   int chunk;
   int64_t chunks;
 };
 
-EmbedWorkspace embed_layout(int64_t n, int64_t dim) {
+EmbedWorkspace embed_layout(int64_t n, int64_t vocab, int64_t dim) {
   EmbedWorkspace w{};
   // A chunk's rows are summed by one wave: fewer of them where there would be too few waves.
   const int64_t tiles = (dim + 511) / 512;
@@ -112,12 +114,15 @@ EmbedWorkspace embed_layout(int64_t n, int64_t dim) {
     w.positions[i] = place(w.total, (size_t)n * 4);
   }
   w.counts = place(w.total, (size_t)kSortGrid * kDigits * 4);
+  w.present = place(w.total, (size_t)vocab);
   w.pieces = place(w.total, (size_t)w.chunks * 2 * dim * 4);
   return w;
 }
 
-// Positions by token, into keys[0] and positions[0] of the workspace.
-void sort_tokens(const TokenKeys& in, char* ws, const EmbedWorkspace& w, hipStream_t stream) {
+constexpr int64_t kSmallSort = 8 * kSortThreads;            // keys that one workgroup sorts
+
+// Positions by token, into keys[0] and positions[0] of the workspace; and which tokens there are, unless `present` is null.
+void sort_tokens(const TokenKeys& in, char* ws, const EmbedWorkspace& w, uint8_t* present, hipStream_t stream) {
   int width = 1;
   while (in.vocab >> width) ++width;                        // of the largest key, which is `vocab`
   const int passes = (width + kDigitBits - 1) / kDigitBits, bits = (width + passes - 1) / passes;
@@ -126,23 +131,23 @@ void sort_tokens(const TokenKeys& in, char* ws, const EmbedWorkspace& w, hipStre
     keys[i] = (uint32_t*)(ws + w.keys[i]);
     positions[i] = (uint32_t*)(ws + w.positions[i]);
   }
-  if (in.n <= 4 * kSortThreads) {
-    hipLaunchKernelGGL(sort_small_kernel<4>, dim3(1), dim3(kSortThreads), 0, stream, in, bits, passes, keys[0], positions[0]);
-    return;
-  }
-  if (in.n <= 8 * kSortThreads) {
-    hipLaunchKernelGGL(sort_small_kernel<8>, dim3(1), dim3(kSortThreads), 0, stream, in, bits, passes, keys[0], positions[0]);
+  if (in.n <= kSmallSort) {
+    const auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(1), dim3(kSortThreads), 0, stream, in, bits, passes, keys[0], positions[0], present);
+    };
+    if (in.n <= 2 * kSortThreads) launch(sort_small_kernel<2>);
+    else launch(sort_small_kernel<8>);
     return;
   }
   uint32_t* counts = (uint32_t*)(ws + w.counts);
-  const int64_t most = (in.n + kSortGrid - 1) / kSortGrid, each = (most + kSortTile - 1) / kSortTile * kSortTile;
+  const int64_t most = (in.n + kSortGrid - 1) / kSortGrid, each = (most + kSortThreads - 1) / kSortThreads * kSortThreads;
   const dim3 grid(blocks(in.n, each));
   for (int p = 0; p < passes; ++p) {
     const int to = (passes - 1 - p) & 1, from = to ^ 1;
     const auto pass = [&](auto count, auto scatter) {
-      hipLaunchKernelGGL(count, grid, dim3(kSortThreads), 0, stream, in, keys[from], p * bits, 1 << bits, each, counts);
+      hipLaunchKernelGGL(count, grid, dim3(kSortThreads), 0, stream, in, keys[from], p * bits, 1 << bits, each, counts, present);
       hipLaunchKernelGGL(scatter, grid, dim3(kSortThreads), 0, stream, in, keys[from], positions[from], p * bits, bits, each, counts,
-                         keys[to], positions[to]);
+                         keys[to], positions[to], present);
     };
     if (p == 0) pass(sort_count_kernel<true>, sort_scatter_kernel<true>);
     else pass(sort_count_kernel<false>, sort_scatter_kernel<false>);
@@ -171,7 +176,13 @@ void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, 
   parts = (vocab + each - 1) / each;
   if (parts == 1) {
     for_rows(n, 1, [&](int64_t first, int64_t rows) {
-      hipLaunchKernelGGL(logprobs_kernel<T>, dim3((unsigned)rows), dim3(256), 0, stream, logits, vocab, stride, first, a);
+      const auto launch = [&](auto kernel, int threads) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, stream, logits, vocab, stride, first, a);
+      };
+      // 32 waves a compute unit, as far as a row has work for them
+      if (n < kParts && steps >= 16) launch(logprobs_kernel<T, 1024>, 1024);
+      else if (n < 2 * kParts && steps >= 8) launch(logprobs_kernel<T, 512>, 512);
+      else launch(logprobs_kernel<T, 256>, 256);
     });
     return;
   }
@@ -200,11 +211,13 @@ void launch_rows(const T* logits, int64_t n, int64_t vocab, int64_t stride, cons
 
 template <typename T>
 void launch_grad(const T* logits, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets, const float* lse,
-                 const float* upstream, T* grad, int64_t grad_stride, hipStream_t stream) {
+                 const float* upstream, T* grad, int64_t grad_stride, hipStream_t stream, const double* losses = nullptr,
+                 int32_t n_losses = 0, float* loss = nullptr) {
   const int64_t parts = (vocab / Vec<T>::kWidth + 1023) / 1024 + (vocab / Vec<T>::kWidth % 1024 == 0 && vocab % Vec<T>::kWidth);
   for_rows(n, parts, [&](int64_t first, int64_t rows) {
-    hipLaunchKernelGGL(logprobs_grad_kernel<T>, dim3((unsigned)(rows * parts)), dim3(256), 0, stream, logits, vocab, stride, first,
-                       (unsigned)parts, targets, lse, upstream, grad, grad_stride);
+    float* const here = first == 0 ? loss : nullptr;
+    hipLaunchKernelGGL(logprobs_grad_kernel<T>, dim3((unsigned)(rows * parts + (here ? 1 : 0))), dim3(256), 0, stream, logits, vocab,
+                       stride, first, (unsigned)parts, targets, lse, upstream, grad, grad_stride, losses, n_losses, here);
   });
 }
 
@@ -227,7 +240,7 @@ int bpe_embed_tokens(const void* weight, int dtype, int64_t vocab, int64_t dim, 
 
 size_t bpe_embed_tokens_grad_workspace_bytes(int64_t n, int64_t vocab, int64_t dim) {
   if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS || dim < 1 || dim > BPE_MAX_COLUMNS) return 0;
-  return embed_layout(n, dim).total;
+  return embed_layout(n, vocab, dim).total;
 }
 
 int bpe_embed_tokens_grad(const void* grad, int dtype, int64_t grad_stride, const int32_t* ids, int64_t n,
@@ -238,9 +251,10 @@ int bpe_embed_tokens_grad(const void* grad, int dtype, int64_t grad_stride, cons
       !fits(ids, n, 4) || !aligned(count, 8) ||
       !is_workspace(workspace, workspace_bytes, bpe_embed_tokens_grad_workspace_bytes(n, vocab, dim)))
     return BPE_EINVAL;
-  const EmbedWorkspace w = embed_layout(n, dim);
+  const EmbedWorkspace w = embed_layout(n, vocab, dim);
   char* ws = (char*)workspace;
-  if (n > 0) sort_tokens({ids, n, count, (uint32_t)vocab}, ws, w, (hipStream_t)stream);
+  uint8_t* present = accumulate ? nullptr : (uint8_t*)(ws + w.present);
+  if (n > 0) sort_tokens({ids, n, count, (uint32_t)vocab}, ws, w, present, (hipStream_t)stream);
   GradArgs a{};
   a.keys = (const uint32_t*)(ws + w.keys[0]);
   a.positions = (const uint32_t*)(ws + w.positions[0]);
@@ -253,6 +267,7 @@ int bpe_embed_tokens_grad(const void* grad, int dtype, int64_t grad_stride, cons
   a.out_stride = out_stride;
   a.scale = scale;
   a.accumulate = accumulate;
+  a.present = present;
   a.pieces = (float*)(ws + w.pieces);
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
@@ -357,16 +372,14 @@ int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab,
   a.lse = lse;
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    if (n > 0) {
-      launch_logprobs((const T*)logits, n, vocab, stride, a, (Stats*)(ws + w.parts), stream);
-      hipLaunchKernelGGL(zero_kernel, dim3(blocks(n, 256)), dim3(256), 0, stream, upstream, n);
-    }
-    if (batch > 0)
-      hipLaunchKernelGGL(pair_kernel, dim3(batch / 2), dim3(256), 0, stream, lp, targets, n, vocab, offsets, batch, reference,
+    if (n > 0) launch_logprobs((const T*)logits, n, vocab, stride, a, (Stats*)(ws + w.parts), stream);
+    if (batch > 0 || n > 0)
+      hipLaunchKernelGGL(pair_kernel, dim3(batch / 2 + 1), dim3(256), 0, stream, lp, targets, n, vocab, offsets, batch, reference,
                          beta, smoothing, scale, margins, losses, upstream);
-    hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(256), 0, stream, losses, (int64_t)(batch / 2), loss);
     if (n > 0)
-      launch_grad((const T*)logits, n, vocab, stride, targets, lse, upstream, (T*)grad, grad_stride, stream);
+      launch_grad((const T*)logits, n, vocab, stride, targets, lse, upstream, (T*)grad, grad_stride, stream, losses, batch / 2, loss);
+    else
+      hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(1024), 0, stream, losses, (int64_t)(batch / 2), loss);
   });
   return launched();
 }
@@ -387,11 +400,14 @@ int bpe_policy_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int
   const hipStream_t stream = (hipStream_t)stream_ptr;
   char* ws = (char*)workspace;
   int32_t* counts = (int32_t*)(ws + w.counts);
+  const unsigned groups = std::min(kWeightGroups, blocks(batch, kWeightWaves));
   RowArgs a{};
   a.targets = targets;
   a.logprobs = logprobs;
   a.grad_stride = grad_stride;
   a.weight = (float*)(ws + w.upstream);
+  a.scored = by_string ? nullptr : counts;
+  a.n_scored = (int)groups;
   a.advantage = (float*)(ws + w.advantage);
   a.old = old;
   a.reference = reference;
@@ -401,15 +417,14 @@ int bpe_policy_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int
   a.scale = scale;
   a.value = (double*)(ws + w.values);
   if (n > 0) {
-    hipLaunchKernelGGL(count_kernel, dim3(1), dim3(256), 0, stream, targets, n, vocab, offsets, batch, counts);
-    hipLaunchKernelGGL(weights_kernel, dim3(blocks(n, 256)), dim3(256), 0, stream, targets, n, vocab, offsets, batch, counts,
-                       by_string, advantages, advantage_by_string, (float*)(ws + w.upstream), (float*)(ws + w.advantage));
+    hipLaunchKernelGGL(weights_kernel, dim3(groups + 1), dim3(64 * kWeightWaves), 0, stream, targets, n, vocab, offsets, batch,
+                       by_string, advantages, advantage_by_string, (float*)(ws + w.upstream), (float*)(ws + w.advantage), counts);
     with_type(dtype, [&](auto type) {
       using T = decltype(type);
       launch_rows<T, kRowPolicy>((const T*)logits, n, vocab, stride, a, (T*)grad, stream);
     });
   }
-  hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(256), 0, stream, a.value, n, loss);
+  hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(1024), 0, stream, a.value, n, loss);
   return launched();
 }
 

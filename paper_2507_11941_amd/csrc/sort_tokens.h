@@ -13,7 +13,12 @@ namespace bpe {
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortGrid = 256;                               // workgroups at most
-constexpr int kSortTile = 4 * kSortThreads;                  // keys a workgroup ranks at a time
+
+// Which tokens there are, a byte each: cleared before any is set.
+__device__ inline void clear_present(uint8_t* present, uint32_t vocab, unsigned part, unsigned parts) {
+  const uint4 none = {0, 0, 0, 0};
+  for (uint32_t i = part * kSortThreads + threadIdx.x; i < (vocab + 15) / 16; i += parts * kSortThreads) ((uint4*)present)[i] = none;
+}
 
 // Where position t's key comes from: the ids, with `vocab` -- behind all tokens -- for padding and what is not in use.
 struct TokenKeys {
@@ -77,7 +82,8 @@ __device__ inline uint32_t scan_digits(uint32_t mine, uint32_t* wave_sum) {
 
 // Up to kEach x 1,024 keys: one workgroup does all passes, the keys in its registers and LDS.
 template <int kEach>
-__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(TokenKeys in, int bits, int passes, uint32_t* keys, uint32_t* positions) {
+__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(TokenKeys in, int bits, int passes, uint32_t* keys, uint32_t* positions,
+                                                                  uint8_t* present) {
   __shared__ uint32_t counter[kSortWaves][kDigits];
   __shared__ uint32_t base[kDigits], wave_sum[kSortWaves];
   __shared__ uint32_t held[kEach * kSortThreads];
@@ -90,9 +96,15 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(TokenKeys in, 
     at[e] = (uint32_t)(first + e * 64);
     key[e] = in.key(at[e], rows);
   }
+  if (present) clear_present(present, in.vocab, 0, 1);
   for (int p = 0; p < passes; ++p) {
-    for (int d = threadIdx.x; d < kSortWaves * kDigits; d += kSortThreads) (&counter[0][0])[d] = 0;
+    for (int d = lane; d < digits; d += 64) counter[wave][d] = 0;
     __syncthreads();
+    if (p == 0 && present) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (key[e] < in.vocab) present[key[e]] = 1;
+    }
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       rank[e] = wave_rank(key[e] >> (p * bits) & (digits - 1), bits, first + e * 64 < n, counter[wave]);
@@ -130,12 +142,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(TokenKeys in, 
     }
 }
 
-// A pass over more: each workgroup has the keys [its number x each, ...), `each` a multiple of kSortTile.  First their counts.
+// A pass over more: each workgroup has the keys [its number x each, ...), `each` a multiple of 1,024.  First their counts.
 template <bool kFirst>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(TokenKeys in, const uint32_t* keys_in, int shift, int digits, int64_t each,
-                                                                  uint32_t* counts) {
+                                                                  uint32_t* counts, uint8_t* present) {
   __shared__ uint32_t count[kDigits];
   for (int d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
+  if (kFirst && present) clear_present(present, in.vocab, blockIdx.x, gridDim.x);
   __syncthreads();
   const int64_t begin = blockIdx.x * each, end = min(in.n, begin + each);
   const int64_t rows = kFirst ? in.rows() : 0;
@@ -147,48 +160,56 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(TokenKeys in, 
   for (int d = threadIdx.x; d < digits; d += kSortThreads) counts[blockIdx.x * kDigits + d] = count[d];
 }
 
+// ... then their places: all smaller digits, the same digit of the workgroups before, and the numbers in this one.
 template <bool kFirst>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(TokenKeys in, const uint32_t* keys_in, const uint32_t* positions_in,
                                                                     int shift, int bits, int64_t each, const uint32_t* counts, uint32_t* keys,
-                                                                    uint32_t* positions) {
-  constexpr int kEach = kSortTile / kSortThreads;
+                                                                    uint32_t* positions, uint8_t* present) {
   __shared__ uint32_t counter[kSortWaves][kDigits];
   __shared__ uint32_t base[kDigits], wave_sum[kSortWaves];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, digits = 1 << bits;
-  uint32_t total = 0, before_me = 0;
-  if ((int)threadIdx.x < digits)
-    for (unsigned b = 0; b < gridDim.x; ++b) {
-      const uint32_t c = counts[b * kDigits + threadIdx.x];
-      total += c;
-      before_me += b < blockIdx.x ? c : 0;
+  // The counts of all workgroups, by as many threads for a digit as there are.
+  const int digit = threadIdx.x & (digits - 1), share = threadIdx.x >> bits, shares = kSortThreads >> bits;
+  uint32_t all = 0, before_me = 0;
+  for (unsigned b0 = share; b0 < gridDim.x; b0 += 32 * shares) {
+    uint32_t c[32];                                          // (side by side: they come from other XCDs' caches, 2 us a read)
+#pragma unroll
+    for (int i = 0; i < 32; ++i) c[i] = b0 + i * shares < gridDim.x ? counts[(b0 + i * shares) * kDigits + digit] : 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      all += c[i];
+      before_me += b0 + i * shares < blockIdx.x ? c[i] : 0;
     }
-  const uint32_t before = scan_digits(total, wave_sum);
-  if ((int)threadIdx.x < digits) base[threadIdx.x] = before + before_me;
+  }
+  uint32_t* part = &counter[0][0];                            // (its 8,192 words are not in use yet)
+  part[threadIdx.x] = all;
+  part[kSortThreads + threadIdx.x] = before_me;
+  __syncthreads();
+  uint32_t total = 0, earlier = 0;
+  if ((int)threadIdx.x < digits)
+    for (int h = 0; h < shares; ++h) {
+      total += part[h * digits + threadIdx.x];
+      earlier += part[kSortThreads + h * digits + threadIdx.x];
+    }
+  const uint32_t before = scan_digits(total, wave_sum);       // (synchronises)
+  if ((int)threadIdx.x < digits) base[threadIdx.x] = before + earlier;
   const int64_t begin = blockIdx.x * each, end = min(in.n, begin + each);
   const int64_t rows = kFirst ? in.rows() : 0;
-  for (int64_t tile = begin; tile < end; tile += kSortTile) {
-    for (int d = threadIdx.x; d < kSortWaves * kDigits; d += kSortThreads) (&counter[0][0])[d] = 0;
-    __syncthreads();
-    const int64_t first = tile + wave * 64 * kEach + lane;
-    uint32_t key[kEach], rank[kEach], at[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int64_t t = first + e * 64;
-      key[e] = kFirst ? in.key(t, rows) : t < end ? keys_in[t] : 0;
-      at[e] = kFirst ? (uint32_t)t : t < end ? positions_in[t] : 0;
-    }
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) rank[e] = wave_rank(key[e] >> shift & (digits - 1), bits, first + e * 64 < end, counter[wave]);
+  for (int64_t t0 = begin; t0 < end; t0 += kSortThreads) {
+    for (int d = lane; d < digits; d += 64) counter[wave][d] = 0;
+    const int64_t t = t0 + threadIdx.x;
+    const uint32_t key = kFirst ? in.key(t, rows) : t < end ? keys_in[t] : 0;
+    const uint32_t at = kFirst ? (uint32_t)t : t < end ? positions_in[t] : 0;
+    const uint32_t rank = wave_rank(key >> shift & (digits - 1), bits, t < end, counter[wave]);
     __syncthreads();
     places_of_waves(counter, base, digits);
     __syncthreads();
-#pragma unroll
-    for (int e = 0; e < kEach; ++e)
-      if (first + e * 64 < end) {
-        const uint32_t to = counter[wave][key[e] >> shift & (digits - 1)] + rank[e];
-        keys[to] = key[e];
-        positions[to] = at[e];
-      }
+    if (t < end) {
+      const uint32_t to = counter[wave][key >> shift & (digits - 1)] + rank;
+      keys[to] = key;
+      positions[to] = at;
+      if (kFirst && present && key < in.vocab) present[key] = 1;
+    }
     __syncthreads();
   }
 }
