@@ -72,6 +72,7 @@ struct GradArgs {
   float scale;
   int accumulate;
   const uint8_t* present;                                    // whether there is a token; not used where it is accumulated
+  uint32_t* long_runs;                                       // their number, cleared by the sort; then the chunks they begin in
   float* pieces;                                             // [chunks][2][dim]: of a run from before, of one that goes on
 };
 
@@ -177,7 +178,12 @@ __global__ void __launch_bounds__(256) embed_grad_kernel(const T* grad, O* out, 
     const uint64_t run = __ballot(key == last_key);
     tail_begin = (int)__builtin_ctzll(run);
     const int end = tail_begin + (int)__builtin_ctzll(~(run >> tail_begin) | ((uint64_t)1 << 63));
-    if (end - tail_begin > a.chunk) tail_piece = true; else to = end;
+    if (end - tail_begin > a.chunk) {
+      tail_piece = true;
+      if (tile == 0 && lane == 0) a.long_runs[1 + atomicAdd(a.long_runs, 1u)] = (uint32_t)c;     // (in any order: each is summed by itself)
+    } else {
+      to = end;
+    }
   }
   if (head_end > 0) from = 0;
   const int n_rows = min(to, (int)__builtin_ctzll(~__ballot(key < a.vocab) | ((uint64_t)1 << 63)));      // (padding is behind all tokens)
@@ -210,56 +216,55 @@ __global__ void __launch_bounds__(256) embed_grad_kernel(const T* grad, O* out, 
   }
 }
 
-// Long runs: one workgroup for the run, if there is one, that begins in a chunk and has more positions than a chunk, and a tile
-// of the columns.  Its four waves add a quarter of the pieces each.
+// Long runs: a workgroup for each and a tile of the columns, as far as there are workgroups.  Its four waves add a quarter of
+// the pieces each.
 template <typename T, typename O>
-__global__ void __launch_bounds__(256) embed_grad_join_kernel(O* out, GradArgs a, int64_t first) {
+__global__ void __launch_bounds__(256) embed_grad_join_kernel(O* out, GradArgs a) {
   constexpr int kWidth = Vec<T>::kWidth;
-  const int64_t c = (first + blockIdx.x) / a.tiles, tile = (first + blockIdx.x) % a.tiles, begin = c * a.chunk, end = begin + a.chunk;
-  if (end >= a.n) return;                                    // (the last chunk's runs end with it)
-  const uint32_t key = a.keys[end - 1];
-  if (key >= a.vocab || a.keys[end] != key) return;
-  if (begin > 0 && a.keys[begin - 1] == key) return;         // it begins before
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t run = __ballot(lane < a.chunk && a.keys[begin + min(lane, a.chunk - 1)] == key);
-  const int64_t start = begin + (int64_t)__builtin_ctzll(run);
-  if (start + a.chunk >= a.n || a.keys[start + a.chunk] != key) return;
-  // The chunks that it goes on into begin with it.
-  int64_t pieces = 1;
-  for (;;) {
-    const int64_t at = (c + pieces + lane) * a.chunk;
-    const uint64_t more = __ballot(at < a.n && a.keys[min(at, a.n - 1)] == key);
-    pieces += more == ~(uint64_t)0 ? 64 : (int)__builtin_ctzll(~more);
-    if (more != ~(uint64_t)0) break;
-  }
-  const int64_t each = (pieces + 3) / 4, last = min(pieces, (wave + 1) * each);
-  const Columns cols = columns_of<T>(tile, a.dim);
   __shared__ float part[4][64][kWidth];
-  float sum[kWidth] = {};
-  if (a.dim >= kWidth) {
-#pragma unroll 4
-    for (int64_t j = wave * each; j < last; ++j) {
-      const float* piece = a.pieces + (2 * (c + j) + (j == 0)) * a.dim + cols.load;
-#pragma unroll
-      for (int h = 0; h < kWidth; h += 4) {
-        float x[4];
-        Vec<float>::load(piece + h).get(x);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[h + i] += x[i];
-      }
+  const int64_t tasks = (int64_t)a.long_runs[0] * a.tiles;
+  for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const int64_t c = a.long_runs[1 + task / a.tiles], tile = task % a.tiles;
+    const uint32_t key = a.keys[(c + 1) * a.chunk - 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // The chunks that it goes on into begin with it.
+    int64_t pieces = 1;
+    for (;;) {
+      const int64_t at = (c + pieces + lane) * a.chunk;
+      const uint64_t more = __ballot(at < a.n && a.keys[min(at, a.n - 1)] == key);
+      pieces += more == ~(uint64_t)0 ? 64 : (int)__builtin_ctzll(~more);
+      if (more != ~(uint64_t)0) break;
     }
-  } else if (cols.own < cols.end) {
-    for (int64_t j = wave * each; j < last; ++j)
-      for (int i = 0; i < kWidth; ++i)
-        if (i < a.dim) sum[i] += a.pieces[(2 * (c + j) + (j == 0)) * a.dim + i];
+    const int64_t each = (pieces + 3) / 4, last = min(pieces, (wave + 1) * each);
+    const Columns cols = columns_of<T>(tile, a.dim);
+    float sum[kWidth] = {};
+    if (a.dim >= kWidth) {
+#pragma unroll 4
+      for (int64_t j = wave * each; j < last; ++j) {
+        const float* piece = a.pieces + (2 * (c + j) + (j == 0)) * a.dim + cols.load;
+#pragma unroll
+        for (int h = 0; h < kWidth; h += 4) {
+          float x[4];
+          Vec<float>::load(piece + h).get(x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[h + i] += x[i];
+        }
+      }
+    } else if (cols.own < cols.end) {
+      for (int64_t j = wave * each; j < last; ++j)
+        for (int i = 0; i < kWidth; ++i)
+          if (i < a.dim) sum[i] += a.pieces[(2 * (c + j) + (j == 0)) * a.dim + i];
+    }
+    __syncthreads();                                           // (what was joined before is read)
+#pragma unroll
+    for (int i = 0; i < kWidth; ++i) part[wave][lane][i] = sum[i];
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int i = 0; i < kWidth; ++i) sum[i] = part[0][lane][i] + part[1][lane][i] + part[2][lane][i] + part[3][lane][i];
+      store_columns(out + (int64_t)key * a.out_stride, cols, sum, a.scale, a.accumulate);
+    }
   }
-#pragma unroll
-  for (int i = 0; i < kWidth; ++i) part[wave][lane][i] = sum[i];
-  __syncthreads();
-  if (wave > 0) return;
-#pragma unroll
-  for (int i = 0; i < kWidth; ++i) sum[i] = part[0][lane][i] + part[1][lane][i] + part[2][lane][i] + part[3][lane][i];
-  store_columns(out + (int64_t)key * a.out_stride, cols, sum, a.scale, a.accumulate);
 }
 
 }  // namespace bpe

@@ -97,7 +97,7 @@ void launch_embed(const T* weight, int64_t vocab, int64_t dim, int64_t weight_st
 
 // The workspace of the embedding's gradient: keys and positions as they are and as the pass before left them.
 struct EmbedWorkspace {
-  size_t keys[2], positions[2], counts, present, pieces, total;
+  size_t keys[2], positions[2], counts, present, long_runs, pieces, total;
   int chunk;
   int64_t chunks;
 };
@@ -115,6 +115,7 @@ EmbedWorkspace embed_layout(int64_t n, int64_t vocab, int64_t dim) {
   }
   w.counts = place(w.total, (size_t)kSortGrid * kDigits * 4);
   w.present = place(w.total, (size_t)vocab);
+  w.long_runs = place(w.total, ((size_t)w.chunks + 1) * 4);
   w.pieces = place(w.total, (size_t)w.chunks * 2 * dim * 4);
   return w;
 }
@@ -133,7 +134,8 @@ void sort_tokens(const TokenKeys& in, char* ws, const EmbedWorkspace& w, uint8_t
   }
   if (in.n <= kSmallSort) {
     const auto launch = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3(1), dim3(kSortThreads), 0, stream, in, bits, passes, keys[0], positions[0], present);
+      hipLaunchKernelGGL(kernel, dim3(1), dim3(kSortThreads), 0, stream, in, bits, passes, keys[0], positions[0], present,
+                         (uint32_t*)(ws + w.long_runs));
     };
     if (in.n <= 2 * kSortThreads) launch(sort_small_kernel<2>);
     else launch(sort_small_kernel<8>);
@@ -145,7 +147,8 @@ void sort_tokens(const TokenKeys& in, char* ws, const EmbedWorkspace& w, uint8_t
   for (int p = 0; p < passes; ++p) {
     const int to = (passes - 1 - p) & 1, from = to ^ 1;
     const auto pass = [&](auto count, auto scatter) {
-      hipLaunchKernelGGL(count, grid, dim3(kSortThreads), 0, stream, in, keys[from], p * bits, 1 << bits, each, counts, present);
+      hipLaunchKernelGGL(count, grid, dim3(kSortThreads), 0, stream, in, keys[from], p * bits, 1 << bits, each, counts, present,
+                         (uint32_t*)(ws + w.long_runs));
       hipLaunchKernelGGL(scatter, grid, dim3(kSortThreads), 0, stream, in, keys[from], positions[from], p * bits, bits, each, counts,
                          keys[to], positions[to], present);
     };
@@ -162,9 +165,10 @@ void launch_embed_grad(const T* grad, O* out, GradArgs a, hipStream_t stream) {
   for (int64_t first = 0; first < waves; first += 4 * kMost)
     hipLaunchKernelGGL((embed_grad_kernel<T, O>), dim3(blocks(std::min(4 * kMost, waves - first), 4)), dim3(256), 0, stream, grad, out, a,
                        first, summing);
-  if (a.chunks < 2) return;
-  for (int64_t first = 0; first < summing; first += kMost)
-    hipLaunchKernelGGL((embed_grad_join_kernel<T, O>), dim3((unsigned)std::min(kMost, summing - first)), dim3(256), 0, stream, out, a, first);
+  const int64_t long_runs = a.n / (a.chunk + 1);            // at most
+  if (long_runs > 0)
+    hipLaunchKernelGGL((embed_grad_join_kernel<T, O>), dim3((unsigned)std::min<int64_t>(kFewWaves, long_runs * a.tiles)), dim3(256), 0, stream,
+                       out, a);
 }
 
 template <typename T>
@@ -270,6 +274,7 @@ int bpe_embed_tokens_grad(const void* grad, int dtype, int64_t grad_stride, cons
   a.scale = scale;
   a.accumulate = accumulate;
   a.present = present;
+  a.long_runs = (uint32_t*)(ws + w.long_runs);
   a.pieces = (float*)(ws + w.pieces);
   with_type(dtype, [&](auto type) {
     using T = decltype(type);

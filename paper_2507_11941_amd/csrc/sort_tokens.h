@@ -80,10 +80,10 @@ __device__ inline uint32_t scan_digits(uint32_t mine, uint32_t* wave_sum) {
   return before + sum - mine;
 }
 
-// Up to kEach x 1,024 keys: one workgroup does all passes, the keys in its registers and LDS.
+// Up to kEach x 1,024 keys (and a word that the caller needs cleared): one workgroup does all passes, the keys in its registers and LDS.
 template <int kEach>
 __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(TokenKeys in, int bits, int passes, uint32_t* keys, uint32_t* positions,
-                                                                  uint8_t* present) {
+                                                                  uint8_t* present, uint32_t* cleared) {
   __shared__ uint32_t counter[kSortWaves][kDigits];
   __shared__ uint32_t base[kDigits], wave_sum[kSortWaves];
   __shared__ uint32_t held[kEach * kSortThreads];
@@ -97,6 +97,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(TokenKeys in, 
     key[e] = in.key(at[e], rows);
   }
   if (present) clear_present(present, in.vocab, 0, 1);
+  if (threadIdx.x == 0) *cleared = 0;
   for (int p = 0; p < passes; ++p) {
     for (int d = lane; d < digits; d += 64) counter[wave][d] = 0;
     __syncthreads();
@@ -145,10 +146,11 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(TokenKeys in, 
 // A pass over more: each workgroup has the keys [its number x each, ...), `each` a multiple of 1,024.  First their counts.
 template <bool kFirst>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(TokenKeys in, const uint32_t* keys_in, int shift, int digits, int64_t each,
-                                                                  uint32_t* counts, uint8_t* present) {
+                                                                  uint32_t* counts, uint8_t* present, uint32_t* cleared) {
   __shared__ uint32_t count[kDigits];
   for (int d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
   if (kFirst && present) clear_present(present, in.vocab, blockIdx.x, gridDim.x);
+  if (kFirst && blockIdx.x == 0 && threadIdx.x == 0) *cleared = 0;
   __syncthreads();
   const int64_t begin = blockIdx.x * each, end = min(in.n, begin + each);
   const int64_t rows = kFirst ? in.rows() : 0;
