@@ -63,9 +63,12 @@ int bpe_next_tokens(const int32_t* ids, int64_t n, const int64_t* offsets, int32
 /* logprobs[t] = logits[t][targets[t]] - lse[t], lse[t] = log(sum over j of exp(logits[t][j])).
  * A row whose target is outside [0, vocab) is not scored: it is not read, whatever it holds, and both outputs are 0.
  * Logits of -inf (masked entries) have probability 0; a row without any finite one has no distribution, and gives NaN.
- *   logits  [n][vocab] of `dtype`;  logprobs, lse float[n], either may be NULL. */
+ *   logits  [n][vocab] of `dtype`;  logprobs, lse float[n], either may be NULL.
+ *   workspace  may be NULL where none is needed. */
 int bpe_token_logprobs(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets,
                        float* logprobs, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+/* Bytes of its workspace: 0 where it needs none (only few rows that are long are split among workgroups). */
+size_t bpe_token_logprobs_workspace_bytes(int64_t n, int64_t vocab);
 
 /* The gradient with respect to the logits of sum over t of upstream[t] * logprobs[t]:
  *   grad[t][j] = upstream[t] * ((j == targets[t]) - exp(logits[t][j] - lse[t])).
@@ -80,11 +83,10 @@ int bpe_token_logprobs_grad(const void* logits, int dtype, int64_t n, int64_t vo
  * A scored row whose upstream is 0 is read for its log-probability, and its gradient is zeros. */
 int bpe_token_logprobs_and_grad(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride,
                                 const int32_t* targets, const float* upstream, float* logprobs, float* lse, void* grad,
-                                int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream);
+                                int64_t grad_stride, void* stream);
 
-/* Bytes of workspace that the functions on logits need: those above with batch = 0, the losses below with theirs.  0 for sizes
- * that are out of range. */
-size_t bpe_logits_workspace_bytes(int64_t n, int64_t vocab, int32_t batch);
+/* Bytes of workspace that the two losses need; 0 for sizes that are out of range. */
+size_t bpe_loss_workspace_bytes(int64_t n, int64_t vocab, int32_t batch);
 
 /* Preference loss on pairs: string 2k is preferred to string 2k+1.  With S_i the sum of logprobs[t] - reference[t] over the
  * scored positions t of string i,

@@ -27,7 +27,7 @@ def _load():
                 "next_tokens": [vp, i64, vp, i32, vp, vp, vp],
                 "token_logprobs": [vp, i, i64, i64, i64, vp, vp, vp, vp, sz, vp],
                 "token_logprobs_grad": [vp, i, i64, i64, i64, vp, vp, vp, vp, i64, vp],
-                "token_logprobs_and_grad": [vp, i, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, sz, vp],
+                "token_logprobs_and_grad": [vp, i, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp],
                 "preference_loss": [vp, i, i64, i64, i64, vp, vp, i32, vp, f, f, f, vp, vp, vp, vp, i64, vp, sz, vp],
                 "policy_loss": [vp, i, i64, i64, i64, vp, vp, i32, vp, vp, i, vp, f, f, f, i, f, vp, vp, vp, i64, vp, sz, vp],
         }.items():
@@ -35,8 +35,10 @@ def _load():
             function.argtypes, function.restype = args, i
         lib.bpe_embed_tokens_grad_workspace_bytes.argtypes = [i64, i64, i64]
         lib.bpe_embed_tokens_grad_workspace_bytes.restype = sz
-        lib.bpe_logits_workspace_bytes.argtypes = [i64, i64, i32]
-        lib.bpe_logits_workspace_bytes.restype = sz
+        lib.bpe_token_logprobs_workspace_bytes.argtypes = [i64, i64]
+        lib.bpe_token_logprobs_workspace_bytes.restype = sz
+        lib.bpe_loss_workspace_bytes.argtypes = [i64, i64, i32]
+        lib.bpe_loss_workspace_bytes.restype = sz
         _TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
         _lib = lib
     return _lib
@@ -179,10 +181,6 @@ def _grad_of(logits, out):
     return out, stride
 
 
-def _logits_workspace(workspace, n, vocab, batch, dev):
-    return _workspace(workspace, _lib.bpe_logits_workspace_bytes(n, vocab, batch), dev, "logits")
-
-
 def token_logprobs(logits, targets, workspace=None, stream=None):
     """(log-probabilities float32 [n] of the int32 targets [n] under logits [n, vocab], logarithms float32 [n] of the rows'
     sums of exponentials).  Rows whose target is outside the vocabulary are not scored: not read, and 0 in both."""
@@ -191,10 +189,11 @@ def token_logprobs(logits, targets, workspace=None, stream=None):
     n, vocab = logits.shape
     targets_ptr = _vector(targets, "targets", dev, torch.int32, n)
     logprobs, lse = torch.empty(n, dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
-    workspace = _logits_workspace(workspace, n, vocab, 0, dev)
+    need = lib.bpe_token_logprobs_workspace_bytes(n, vocab)
+    workspace = _workspace(workspace, need, dev, "token_logprobs") if need else None
     _enqueue("token_logprobs", dev, stream, (logits, targets, logprobs, lse, workspace), lambda s: lib.bpe_token_logprobs(
         logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, logprobs.data_ptr(), lse.data_ptr(),
-        workspace.data_ptr(), workspace.numel(), s))
+        _pointer(workspace), need, s))
     return logprobs, lse
 
 
@@ -213,7 +212,7 @@ def token_logprobs_grad(logits, targets, lse, upstream, out=None, stream=None):
     return out
 
 
-def token_logprobs_and_grad(logits, targets, upstream, out=None, workspace=None, stream=None):
+def token_logprobs_and_grad(logits, targets, upstream, out=None, stream=None):
     """(logprobs, lse, gradient of ``(upstream * logprobs).sum()``) in one pass over the logits, for an upstream that is known
     before: of cross entropy it is -1 / (number of scored tokens).  ``out`` may be ``logits`` itself."""
     lib = _lib or _load()
@@ -223,11 +222,10 @@ def token_logprobs_and_grad(logits, targets, upstream, out=None, workspace=None,
     upstream_ptr = _vector(upstream, "upstream", dev, torch.float32, n)
     logprobs, lse = torch.empty(n, dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
     out, out_stride = _grad_of(logits, out)
-    workspace = _logits_workspace(workspace, n, vocab, 0, dev)
-    _enqueue("token_logprobs_and_grad", dev, stream, (logits, targets, upstream, logprobs, lse, out, workspace),
+    _enqueue("token_logprobs_and_grad", dev, stream, (logits, targets, upstream, logprobs, lse, out),
              lambda s: lib.bpe_token_logprobs_and_grad(
                  logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, upstream_ptr, logprobs.data_ptr(),
-                 lse.data_ptr(), out.data_ptr(), out_stride, workspace.data_ptr(), workspace.numel(), s))
+                 lse.data_ptr(), out.data_ptr(), out_stride, s))
     return logprobs, lse, out
 
 
@@ -247,7 +245,7 @@ def preference_loss(logits, targets, offsets, reference=None, beta: float = 0.1,
     loss, margins = torch.empty((), dtype=torch.float32, device=dev), torch.empty(batch // 2, dtype=torch.float32, device=dev)
     logprobs = torch.empty(n, dtype=torch.float32, device=dev)
     out, out_stride = _grad_of(logits, out)
-    workspace = _logits_workspace(workspace, n, vocab, batch, dev)
+    workspace = _workspace(workspace, lib.bpe_loss_workspace_bytes(n, vocab, batch), dev, "logits")
     _enqueue("preference_loss", dev, stream, (logits, targets, offsets, reference, loss, margins, logprobs, out, workspace),
              lambda s: lib.bpe_preference_loss(
                  logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, offsets_ptr, batch, reference_ptr,
@@ -277,7 +275,7 @@ def policy_loss(logits, targets, offsets, old, advantages, reference=None, clip_
     reference_ptr = None if reference is None else _vector(reference, "reference", dev, torch.float32, n)
     loss, logprobs = torch.empty((), dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
     out, out_stride = _grad_of(logits, out)
-    workspace = _logits_workspace(workspace, n, vocab, batch, dev)
+    workspace = _workspace(workspace, lib.bpe_loss_workspace_bytes(n, vocab, batch), dev, "logits")
     _enqueue("policy_loss", dev, stream, (logits, targets, offsets, old, advantages, reference, loss, logprobs, out, workspace),
              lambda s: lib.bpe_policy_loss(
                  logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, offsets_ptr, batch, old_ptr,

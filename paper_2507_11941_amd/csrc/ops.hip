@@ -57,12 +57,24 @@ struct LogitsWorkspace {
 
 constexpr unsigned kWeightGroups = 256;                     // workgroups that count scored positions
 
-// Statistics of parts of rows: fewer than this many, and one for each row.
+// Few long rows are split among workgroups, as many as to make about kParts of them in all, and a second launch joins them.
+// Each has 4 KiB of a row in one step.  Of 8 rows of 126, 196, 392 and 3,906 KiB the log-probabilities take 5.8, 6.2, 6.5 and
+// 13.2 us in a graph, each by one workgroup 4.4, 9.8, 9.3 and 85; called one by one, where a launch costs the host 3.4 us,
+// 12.4, 12.1, 11.9 and 12.8 against 9.7, 9.8, 9.3 and 85.  100 rows: called one by one 12.7, 11.9, 13.3, 75 against 9.6, 11.4,
+// 16.3 and 110; 250 rows 12.2, 16.7 and 24.4 against 9.4, 14.9 and 21.3.
 constexpr int64_t kParts = 1024;
+constexpr int64_t kSplitBelow = 200, kSplitFrom = 64;       // rows; steps
 
-LogitsWorkspace logits_layout(int64_t n, int32_t batch) {
+bool splits_rows(int64_t n, int64_t steps) { return n < kSplitBelow && steps > kSplitFrom; }
+
+// ... for the type with the longest rows.
+size_t parts_bytes(int64_t n, int64_t vocab) {
+  return n > 0 && splits_rows(n, (vocab + 1023) / 1024) ? (size_t)(n + kParts) * sizeof(Stats) : 0;
+}
+
+LogitsWorkspace logits_layout(int64_t n, int64_t vocab, int32_t batch) {
   LogitsWorkspace w{};
-  w.parts = place(w.total, (size_t)(n + kParts) * sizeof(Stats));
+  w.parts = place(w.total, parts_bytes(n, vocab));
   w.logprobs = place(w.total, (size_t)n * 8);
   w.values = place(w.total, (size_t)std::max<int64_t>(n, batch) * 8);
   w.upstream = place(w.total, (size_t)n * 4);
@@ -175,7 +187,7 @@ template <typename T>
 void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, const RowArgs& a, Stats* part, hipStream_t stream) {
   constexpr int64_t kStep = 256 * Vec<T>::kWidth;           // 4 KiB of a row
   const int64_t steps = (vocab + kStep - 1) / kStep;
-  int64_t parts = n < kParts / 2 ? std::min(kParts / n, (steps + 1) / 2) : 1;
+  int64_t parts = splits_rows(n, steps) ? std::min(kParts / n, (steps + 1) / 2) : 1;
   const int64_t each = (steps + parts - 1) / parts * kStep;
   parts = (vocab + each - 1) / each;
   if (parts == 1) {
@@ -299,16 +311,22 @@ int bpe_next_tokens(const int32_t* ids, int64_t n, const int64_t* offsets, int32
   return launched();
 }
 
-size_t bpe_logits_workspace_bytes(int64_t n, int64_t vocab, int32_t batch) {
+size_t bpe_loss_workspace_bytes(int64_t n, int64_t vocab, int32_t batch) {
   if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS || batch < 0) return 0;
-  return logits_layout(n, batch).total;
+  return logits_layout(n, vocab, batch).total;
+}
+
+size_t bpe_token_logprobs_workspace_bytes(int64_t n, int64_t vocab) {
+  if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS) return 0;
+  return parts_bytes(n, vocab);
 }
 
 int bpe_token_logprobs(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets,
                        float* logprobs, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   if (!is_count(n) || !is_matrix(logits, dtype, n, vocab, stride) || !fits(targets, n, 4) || !aligned(logprobs, 4) ||
-      !aligned(lse, 4) || !is_workspace(workspace, workspace_bytes, bpe_logits_workspace_bytes(n, vocab, 0)))
+      !aligned(lse, 4))
     return BPE_EINVAL;
+  if (parts_bytes(n, vocab) && !is_workspace(workspace, workspace_bytes, parts_bytes(n, vocab))) return BPE_EINVAL;
   if (n == 0) return BPE_OK;
   RowArgs a{};
   a.targets = targets;
@@ -316,7 +334,7 @@ int bpe_token_logprobs(const void* logits, int dtype, int64_t n, int64_t vocab, 
   a.lse = lse;
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    launch_logprobs((const T*)logits, n, vocab, stride, a, (Stats*)((char*)workspace + logits_layout(n, 0).parts), (hipStream_t)stream);
+    launch_logprobs((const T*)logits, n, vocab, stride, a, (Stats*)workspace, (hipStream_t)stream);
   });
   return launched();
 }
@@ -336,10 +354,9 @@ int bpe_token_logprobs_grad(const void* logits, int dtype, int64_t n, int64_t vo
 
 int bpe_token_logprobs_and_grad(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride,
                                 const int32_t* targets, const float* upstream, float* logprobs, float* lse, void* grad,
-                                int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream) {
+                                int64_t grad_stride, void* stream) {
   if (!is_count(n) || !is_matrix(logits, dtype, n, vocab, stride) || !is_matrix(grad, dtype, n, vocab, grad_stride) ||
-      !fits(targets, n, 4) || !fits(upstream, n, 4) || !aligned(logprobs, 4) || !aligned(lse, 4) ||
-      !is_workspace(workspace, workspace_bytes, bpe_logits_workspace_bytes(n, vocab, 0)))
+      !fits(targets, n, 4) || !fits(upstream, n, 4) || !aligned(logprobs, 4) || !aligned(lse, 4))
     return BPE_EINVAL;
   if (n == 0) return BPE_OK;
   RowArgs a{};
@@ -363,9 +380,9 @@ int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab,
       batch < 0 || batch % 2 || !fits(targets, n, 4) || !offsets || !aligned(offsets, 8) || !aligned(reference, 4) ||
       !std::isfinite(beta) || !(smoothing >= 0.0f && smoothing <= 1.0f) || !std::isfinite(scale) || !loss || !aligned(loss, 4) ||
       !aligned(margins, 4) || !aligned(logprobs, 4) ||
-      !is_workspace(workspace, workspace_bytes, bpe_logits_workspace_bytes(n, vocab, batch)))
+      !is_workspace(workspace, workspace_bytes, bpe_loss_workspace_bytes(n, vocab, batch)))
     return BPE_EINVAL;
-  const LogitsWorkspace w = logits_layout(n, batch);
+  const LogitsWorkspace w = logits_layout(n, vocab, batch);
   const hipStream_t stream = (hipStream_t)stream_ptr;
   char* ws = (char*)workspace;
   double* lp = (double*)(ws + w.logprobs);
@@ -401,9 +418,9 @@ int bpe_policy_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int
       !fits(advantages, advantage_by_string ? batch : n, 4) || !aligned(reference, 4) || !(clip_low >= 0.0f && clip_low <= 1.0f) ||
       !(clip_high >= 0.0f && std::isfinite(clip_high)) || !(kl_weight >= 0.0f && std::isfinite(kl_weight)) || !std::isfinite(scale) ||
       !loss || !aligned(loss, 4) || !aligned(logprobs, 4) ||
-      !is_workspace(workspace, workspace_bytes, bpe_logits_workspace_bytes(n, vocab, batch)))
+      !is_workspace(workspace, workspace_bytes, bpe_loss_workspace_bytes(n, vocab, batch)))
     return BPE_EINVAL;
-  const LogitsWorkspace w = logits_layout(n, batch);
+  const LogitsWorkspace w = logits_layout(n, vocab, batch);
   const hipStream_t stream = (hipStream_t)stream_ptr;
   char* ws = (char*)workspace;
   int32_t* counts = (int32_t*)(ws + w.counts);

@@ -240,7 +240,7 @@ def test_refusals():
     for bad in (lambda: bpe.token_logprobs(x.cpu(), targets), lambda: bpe.token_logprobs(x, targets.long()), lambda: bpe.token_logprobs(x, targets[:3]),
                 lambda: bpe.token_logprobs(x.double(), targets), lambda: bpe.token_logprobs(x.t(), some_targets(10, 4, 1)),
                 lambda: bpe.token_logprobs(x[:, :0], targets), lambda: bpe.token_logprobs(x[0], targets),
-                lambda: bpe.token_logprobs(x, targets, workspace=torch.empty(1, dtype=torch.uint8, device=dev())),
+                lambda: bpe.token_logprobs(some_logits(4, 100260, torch.float32, 1), targets, workspace=torch.empty(1, dtype=torch.uint8, device=dev())),
                 lambda: bpe.token_logprobs_grad(x, targets, u, u[:3]), lambda: bpe.token_logprobs_grad(x, targets, u.double(), u),
                 lambda: bpe.token_logprobs_grad(x, targets, u, u, out=x.half()), lambda: bpe.token_logprobs_and_grad(x, targets, u.cpu()),
                 lambda: bpe.token_logprobs_and_grad(x, targets, u, out=torch.empty(4, 11, device=dev())),

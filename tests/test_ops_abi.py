@@ -13,7 +13,7 @@ A = 1 << 20                                              # an address that is al
 def test_library_exports_every_declared_symbol():
     text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "bpe_ops.h")).read(), flags=re.S)
     names = sorted(set(re.findall(r"\b(bpe_[a-z_0-9]+)\s*\(", text)))
-    assert len(names) == 10
+    assert len(names) == 11
     for name in names:
         assert hasattr(bpe.load_library(), name), name
 
@@ -50,11 +50,13 @@ def test_embedding_arguments():
 
 
 def test_logits_arguments():
-    call("token_logprobs", dict(LOGITS, logprobs=A, lse=A, **WORK), [*BAD_LOGITS, ("logprobs", A + 2), ("lse", A + 1), *BAD_WORK])
+    call("token_logprobs", dict(LOGITS, logprobs=A, lse=A, **WORK), [*BAD_LOGITS, ("logprobs", A + 2), ("lse", A + 1)])
+    long_rows = dict(LOGITS, vocab=100260, stride=100260, logprobs=A, lse=A, **WORK)
+    call("token_logprobs", long_rows, BAD_WORK)
     call("token_logprobs_grad", dict(LOGITS, lse=A, upstream=A, grad=A, grad_stride=7, stream=None),
          [*BAD_LOGITS, ("lse", None), ("upstream", None), ("upstream", A + 1), *BAD_GRAD])
-    call("token_logprobs_and_grad", dict(LOGITS, upstream=A, logprobs=A, lse=A, grad=A, grad_stride=7, **WORK),
-         [*BAD_LOGITS, ("upstream", None), ("logprobs", A + 1), ("lse", A + 1), *BAD_GRAD, *BAD_WORK])
+    call("token_logprobs_and_grad", dict(LOGITS, upstream=A, logprobs=A, lse=A, grad=A, grad_stride=7, stream=None),
+         [*BAD_LOGITS, ("upstream", None), ("logprobs", A + 1), ("lse", A + 1), *BAD_GRAD])
     call("next_tokens", dict(ids=A, n=3, offsets=A, batch=2, first=None, targets=A, stream=None),
          [("ids", None), ("ids", A + 1), ("n", -1), ("offsets", None), ("offsets", A + 4), ("batch", -1), ("first", A + 1), ("targets", None)])
 
@@ -78,11 +80,12 @@ def test_workspaces():
     for n, vocab, dim in ((-1, 5, 5), (5, 0, 5), (5, 5, 0), (1 << 30, 5, 5), (5, BIG, 5), (5, 5, BIG)):
         assert lib.bpe_embed_tokens_grad_workspace_bytes(n, vocab, dim) == 0
     for n, vocab, batch in ((-1, 5, 0), (5, 0, 0), (5, 5, -1), (1 << 30, 5, 0)):
-        assert lib.bpe_logits_workspace_bytes(n, vocab, batch) == 0
+        assert lib.bpe_loss_workspace_bytes(n, vocab, batch) == 0
     for n in (0, 1, 1000, 100000):
         assert lib.bpe_embed_tokens_grad_workspace_bytes(n, 100260, 513) > 0
-        assert lib.bpe_logits_workspace_bytes(n, 100260, 0) > 0
-        assert lib.bpe_logits_workspace_bytes(n, 100260, 64) >= lib.bpe_logits_workspace_bytes(n, 100260, 0)
+        assert lib.bpe_loss_workspace_bytes(n, 100260, 64) >= lib.bpe_loss_workspace_bytes(n, 100260, 0) > 0
+    assert lib.bpe_token_logprobs_workspace_bytes(8, 1256) == lib.bpe_token_logprobs_workspace_bytes(0, 100260) == 0
+    assert lib.bpe_token_logprobs_workspace_bytes(8, 100260) > 0
 
 
 def test_tensors_that_are_not_on_the_gpu_are_refused():
