@@ -108,7 +108,7 @@ int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab,
  * and loss = sum of w_t l_t, where w_t = 1 / (scored positions of the batch) or, with `by_string`, 1 / (batch * scored
  * positions of its string).  Where the clipped term is the smaller one the gradient has no part of it.
  *   advantages  float[n], or float[batch] with advantage_by_string != 0: one for all of a string.
- *   reference   float[n], or NULL: no KL term.
+ *   reference   float[n], or NULL: no KL term, and none where kl_weight is 0.
  *   old, reference and advantages are not read where a row is not scored; positions outside every string are not scored.
  *   scale, loss, logprobs, grad  as for bpe_preference_loss (but logprobs are 0 outside every string); loss = 0 where nothing
  *                                is scored. */

@@ -466,8 +466,8 @@ __global__ void __launch_bounds__(1024) sum_kernel(const double* values, int64_t
   sum_values<1024>(values, n, sum);
 }
 
-constexpr int kWeightWaves = 16;                             // strings of a workgroup
-constexpr int kShortString = 4096;                           // positions that one wave goes over
+constexpr int kWeightWaves = 4;                              // strings of a workgroup
+constexpr int kShortString = 512;                            // positions that one wave goes over
 
 // The weight of each scored position in its string's loss and its advantage; and the number of scored positions of this
 // workgroup's strings.  A wave has a string, the whole workgroup one after the other those that are long.  The last workgroup:

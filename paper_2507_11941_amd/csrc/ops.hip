@@ -434,7 +434,7 @@ int bpe_policy_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int
   a.n_scored = (int)groups;
   a.advantage = (float*)(ws + w.advantage);
   a.old = old;
-  a.reference = reference;
+  a.reference = kl_weight > 0.0f ? reference : nullptr;
   a.low = clip_low;
   a.high = clip_high;
   a.kl_weight = kl_weight;
