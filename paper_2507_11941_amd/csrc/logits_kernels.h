@@ -15,11 +15,24 @@ __device__ inline float reference_of(float m) { return m == -INFINITY ? 0.0f : m
 // exp(x - r).  The difference first: a multiple of the type's lowest value would be -inf, and -inf minus itself NaN.
 __device__ inline float exp_of(float x, float r) { return __builtin_amdgcn_exp2f((x - r) * kLog2e); }
 
+// The same for term i of a sum.  log2 e lies between two 32-bit numbers, 1.34e-8 of itself above the one and 6.93e-8 below the
+// other.  With the nearer one alone all terms would be too large, and log-probabilities 1e-7 too low on average, which strings add
+// up; every sixth term takes the other, which makes up for it (a second product would cost 4 % of 8,191 x 100,260's 264 us).
+__device__ inline float term_of(float x, float r, int i) {
+  return __builtin_amdgcn_exp2f((x - r) * (i % 6 ? 1.44269502162933349609f : 1.44269514083862304688f));
+}
+
+// The same for a sum so far: log2 e in two parts.
+__device__ inline float change_of(float m, float r) {
+  const float d = m - r;
+  return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * 1.92596299112661746887e-8f));
+}
+
 // (Both sides the same whichever of them is whose: no product is fused with the addition.)
 __device__ inline Stats join(Stats a, Stats b) {
 #pragma clang fp contract(off)
   const float m = fmaxf(a.m, b.m), r = reference_of(m);
-  return {m, a.s * exp_of(a.m, r) + b.s * exp_of(b.m, r)};
+  return {m, a.s * change_of(a.m, r) + b.s * change_of(b.m, r)};
 }
 
 // Some more of a row's logits: one maximum and one change of reference for all of them.
@@ -35,15 +48,15 @@ __device__ inline void absorb(Stats& stats, const Vec<T>* v) {
     for (int i = 0; i < kWidth; i += 2) m = max_of(m, x[i], x[i + 1]);
   }
   const float r = reference_of(m);
-  float s0 = stats.s * exp_of(stats.m, r), s1 = 0.0f;
+  float s0 = stats.s * change_of(stats.m, r), s1 = 0.0f;
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) {
     float x[kWidth];
     v[k].get(x);
 #pragma unroll
     for (int i = 0; i < kWidth; i += 2) {
-      s0 += exp_of(x[i], r);
-      s1 += exp_of(x[i + 1], r);
+      s0 += term_of(x[i], r, k * kWidth + i);
+      s1 += term_of(x[i + 1], r, k * kWidth + i + 1);
     }
   }
   stats = {m, s0 + s1};
@@ -88,9 +101,13 @@ __device__ inline Stats stream(const T* x, int64_t begin, int64_t end) {
   return stats;
 }
 
-// The logarithm of a token's probability, in 64 bits: x - m is exact or nearly so, and the logarithm's rounding to 32 bits
-// (5e-7 at 10) would be the largest error of a loss that adds up thousands of them.
-__device__ inline double logprob_of(float x, Stats all) { return (double)(x - all.m) - log((double)all.s); }
+// The logarithm of a token's probability.  The difference first, which is exact or nearly so: of logits that are all the type's
+// lowest value m + log s keeps nothing of s.  The logarithm is 32-bit (1.4e-7 below its value on average, 2.4e-7 in the mean
+// square), like that of reference and old log-probabilities from elsewhere, in whose differences to these its lean goes away again:
+// margins of pairs of some hundreds of tokens come out 1e-5 of themselves from 64 bits, and 4e-6 from 32-bit torch on this device.
+__device__ inline float logprob_of(float x, Stats all) { return (x - all.m) - logf(all.s); }
+
+__device__ inline float lse_of(Stats all) { return all.m + logf(all.s); }
 
 enum RowKind { kRowLogprob, kRowStep, kRowPolicy };
 
@@ -98,7 +115,6 @@ struct RowArgs {
   const int32_t* targets;
   float* logprobs;            // null: not wanted
   float* lse;                 // null: not wanted
-  double* logprobs64;         // null: not wanted
   const float* upstream;      // kRowStep
   int64_t grad_stride;
   // kRowPolicy
@@ -113,14 +129,14 @@ struct RowArgs {
 };
 
 // The loss of one token under the clipped policy, and its derivative with respect to the token's log-probability.
-__device__ inline float policy_value(const RowArgs& a, int64_t t, double lp, float* slope) {
+__device__ inline float policy_value(const RowArgs& a, int64_t t, float lp, float* slope) {
   const float advantage = a.advantage[t];
-  const float ratio = expf((float)(lp - (double)a.old[t]));
+  const float ratio = expf(lp - a.old[t]);
   const float free = ratio * advantage, clipped = fminf(fmaxf(ratio, 1.0f - a.low), 1.0f + a.high) * advantage;
   float value = -fminf(free, clipped);
   *slope = free <= clipped ? -free : 0.0f;
   if (a.reference) {
-    const float d = (float)((double)a.reference[t] - lp);
+    const float d = a.reference[t] - lp;
     value += a.kl_weight * (expm1f(d) - d);
     *slope -= a.kl_weight * expm1f(d);
   }
@@ -129,11 +145,10 @@ __device__ inline float policy_value(const RowArgs& a, int64_t t, double lp, flo
 
 // What a row's log-probability gives besides: the outputs of thread 0, and the factor of the row's gradient.
 template <int kKind>
-__device__ inline float finish_row(const RowArgs& a, int64_t t, float weight, Stats all, double lp) {
+__device__ inline float finish_row(const RowArgs& a, int64_t t, float weight, Stats all, float lp) {
   if (threadIdx.x == 0) {
-    if (a.logprobs) a.logprobs[t] = (float)lp;
-    if (a.lse) a.lse[t] = (float)((double)all.m + log((double)all.s));
-    if (a.logprobs64) a.logprobs64[t] = lp;
+    if (a.logprobs) a.logprobs[t] = lp;
+    if (a.lse) a.lse[t] = lse_of(all);
   }
   if constexpr (kKind == kRowStep) return a.upstream[t];
   if constexpr (kKind == kRowPolicy) {
@@ -150,7 +165,6 @@ __device__ inline void skip_row(const RowArgs& a, int64_t t) {
   if (threadIdx.x == 0) {
     if (a.logprobs) a.logprobs[t] = 0.0f;
     if (a.lse) a.lse[t] = 0.0f;
-    if (a.logprobs64) a.logprobs64[t] = 0.0;
     if (kKind == kRowPolicy) a.value[t] = 0.0;
   }
 }
@@ -258,11 +272,11 @@ __global__ void __launch_bounds__(kThreads, kWaves) row_kernel(const T* logits, 
   if constexpr (kVecs % kDeep) absorb<T, kVecs % kDeep>(mine, v + kVecs / kDeep * kDeep);
   const Stats all = join_workgroup<kThreads>(join(mine, {last, 1.0f}));
   if (threadIdx.x < 64) {
-    const double lp = logprob_of(at_target, all);
+    const float lp = logprob_of(at_target, all);
     const float c = finish_row<kKind>(a, t, weight, all, lp);
     if (threadIdx.x == 0) {
       factor[0] = c;
-      factor[1] = -c * expm1f((float)lp);                   // the gradient at the target: 1 - p without the cancellation
+      factor[1] = -c * expm1f(lp);                   // the gradient at the target: 1 - p without the cancellation
     }
   }
   __syncthreads();
@@ -298,11 +312,11 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const T* logits, int64_t
   const float at_target = to_float(x[target]);
   const Stats all = join_workgroup<kThreads>(stream<T, kThreads>(x, 0, vocab));
   if (threadIdx.x < 64) {
-    const double lp = logprob_of(at_target, all);
+    const float lp = logprob_of(at_target, all);
     const float c = finish_row<kKind>(a, t, weight, all, lp);
     if (threadIdx.x == 0) {
       factor[0] = c;
-      factor[1] = -c * expm1f((float)lp);                   // the gradient at the target: 1 - p without the cancellation
+      factor[1] = -c * expm1f(lp);                   // the gradient at the target: 1 - p without the cancellation
     }
   }
   __syncthreads();
@@ -435,7 +449,7 @@ __device__ inline void rows_outside(const int64_t* offsets, int32_t batch, int64
 }
 
 // One workgroup a pair: both sides' sums, the loss, and the factor of each row's gradient.  One more: rows outside every string.
-__global__ void __launch_bounds__(256) pair_kernel(const double* logprobs, const int32_t* targets, int64_t n, int64_t vocab,
+__global__ void __launch_bounds__(256) pair_kernel(const float* logprobs, const int32_t* targets, int64_t n, int64_t vocab,
                                                    const int64_t* offsets, int32_t batch, const float* reference, float beta,
                                                    float smoothing, float scale, float* margins, double* losses, float* upstream) {
   const int32_t k = blockIdx.x;
@@ -446,7 +460,7 @@ __global__ void __launch_bounds__(256) pair_kernel(const double* logprobs, const
   double sum = 0.0;
   for (int64_t t = begin + threadIdx.x; t < end; t += 256)
     if (is_scored(targets, t, vocab)) {
-      const double apart = logprobs[t] - (reference ? (double)reference[t] : 0.0);
+      const double apart = (double)logprobs[t] - (reference ? (double)reference[t] : 0.0);
       sum += t < middle ? apart : -apart;
     }
   const double z = (double)beta * sum_workgroup<256>(sum);

@@ -75,7 +75,7 @@ size_t parts_bytes(int64_t n, int64_t vocab) {
 LogitsWorkspace logits_layout(int64_t n, int64_t vocab, int32_t batch) {
   LogitsWorkspace w{};
   w.parts = place(w.total, parts_bytes(n, vocab));
-  w.logprobs = place(w.total, (size_t)n * 8);
+  w.logprobs = place(w.total, (size_t)n * 4);
   w.values = place(w.total, (size_t)std::max<int64_t>(n, batch) * 8);
   w.upstream = place(w.total, (size_t)n * 4);
   w.advantage = place(w.total, (size_t)n * 4);
@@ -385,14 +385,13 @@ int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab,
   const LogitsWorkspace w = logits_layout(n, vocab, batch);
   const hipStream_t stream = (hipStream_t)stream_ptr;
   char* ws = (char*)workspace;
-  double* lp = (double*)(ws + w.logprobs);
+  float* lp = logprobs ? logprobs : (float*)(ws + w.logprobs);
   double* losses = (double*)(ws + w.values);
   float* upstream = (float*)(ws + w.upstream);
   float* lse = (float*)(ws + w.advantage);
   RowArgs a{};
   a.targets = targets;
-  a.logprobs = logprobs;
-  a.logprobs64 = lp;
+  a.logprobs = lp;
   a.lse = lse;
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
