@@ -132,8 +132,6 @@ EmbedWorkspace embed_layout(int64_t n, int64_t vocab, int64_t dim) {
   return w;
 }
 
-constexpr int64_t kSmallSort = 8 * kSortThreads;            // keys that one workgroup sorts
-
 // Positions by token, into keys[0] and positions[0] of the workspace; and which tokens there are, unless `present` is null.
 void sort_tokens(const TokenKeys& in, char* ws, const EmbedWorkspace& w, uint8_t* present, hipStream_t stream) {
   int width = 1;
@@ -144,13 +142,10 @@ void sort_tokens(const TokenKeys& in, char* ws, const EmbedWorkspace& w, uint8_t
     keys[i] = (uint32_t*)(ws + w.keys[i]);
     positions[i] = (uint32_t*)(ws + w.positions[i]);
   }
-  if (in.n <= kSmallSort) {
-    const auto launch = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3(1), dim3(kSortThreads), 0, stream, in, bits, passes, keys[0], positions[0], present,
-                         (uint32_t*)(ws + w.long_runs));
-    };
-    if (in.n <= 2 * kSortThreads) launch(sort_small_kernel<2>);
-    else launch(sort_small_kernel<8>);
+  if (in.n <= kRankKeys && width + kRankBits <= 32) {
+    const unsigned grid = std::max(blocks(in.n, kRankEach), blocks(in.vocab, kRankTokens));
+    hipLaunchKernelGGL(sort_rank_kernel, dim3(grid), dim3(kRankThreads), 0, stream, in, (blocks(in.vocab, grid) + 15) & ~15u, keys[0],
+                       positions[0], present, (uint32_t*)(ws + w.long_runs));
     return;
   }
   uint32_t* counts = (uint32_t*)(ws + w.counts);

@@ -1,6 +1,7 @@
-// Positions sorted by token: a stable radix sort of n keys below 2^31, digits of at most 9 bits, lowest first.
+// Positions sorted by token, equal tokens in their order: few keys by counting for each of them which are smaller, more by a radix
+// sort of keys below 2^31, digits of at most 9 bits, lowest first.
 //
-// Every wave ranks 64 keys at a time: the lanes that hold the same digit find each other with one ballot per bit, the lowest of
+// In the radix sort every wave ranks 64 keys at a time: the lanes that hold the same digit find each other with one ballot per bit, the lowest of
 // them takes their numbers from the wave's counter of the digit, and a scan over the workgroup's waves (and, through counts in
 // memory, over the workgroups before it) says where each wave's numbers begin.  So equal digits keep their order, whatever the
 // order in which waves run.
@@ -80,67 +81,70 @@ __device__ inline uint32_t scan_digits(uint32_t mine, uint32_t* wave_sum) {
   return before + sum - mine;
 }
 
-// Up to kEach x 1,024 keys (and a word that the caller needs cleared): one workgroup does all passes, the keys in its registers and LDS.
-template <int kEach>
-__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(TokenKeys in, int bits, int passes, uint32_t* keys, uint32_t* positions,
-                                                                  uint8_t* present, uint32_t* cleared) {
-  __shared__ uint32_t counter[kSortWaves][kDigits];
-  __shared__ uint32_t base[kDigits], wave_sum[kSortWaves];
-  __shared__ uint32_t held[kEach * kSortThreads];
-  __shared__ uint16_t held_at[kEach * kSortThreads];
-  const int n = (int)in.n, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = wave * 64 * kEach + lane, digits = 1 << bits;
+// Up to 8,192 keys below 2^19: a key's place is the number of smaller ones, keys and positions taken together as one number, so
+// that no two are equal.  Every workgroup holds all of them in LDS and counts for 32, a wave for four at a time.  n^2 comparisons, but in
+// one launch and with nobody to wait for: 1,000, 2,048, 4,096 and 8,192 keys in 4.5, 6.6, 12 and 16 us, where one workgroup that
+// sorted them by digits took 7, 8.5, 18 and 22, and four launches that do take 8,193 in 21.  Each workgroup also marks which of its share of the tokens there are; and a word that the caller needs is cleared.
+constexpr int kRankKeys = 8192, kRankThreads = 512, kRankWave = 4, kRankEach = kRankThreads / 64 * kRankWave, kRankTokens = 8192;
+constexpr int kRankBits = 13;                                // of a position
+
+__global__ void __launch_bounds__(kRankThreads) sort_rank_kernel(TokenKeys in, uint32_t share, uint32_t* keys, uint32_t* positions,
+                                                                 uint8_t* present, uint32_t* cleared) {
+  __shared__ __align__(16) uint32_t held[kRankKeys];
+  __shared__ __align__(16) uint8_t mark[kRankTokens];
+  const int n = (int)in.n, padded = (n + 255) & ~255;
   const int64_t rows = in.rows();
-  uint32_t key[kEach], at[kEach], rank[kEach];
+  uint32_t loaded[kRankKeys / kRankThreads];                  // (side by side)
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    at[e] = (uint32_t)(first + e * 64);
-    key[e] = in.key(at[e], rows);
-  }
-  if (present) clear_present(present, in.vocab, 0, 1);
-  if (threadIdx.x == 0) *cleared = 0;
-  for (int p = 0; p < passes; ++p) {
-    for (int d = lane; d < digits; d += 64) counter[wave][d] = 0;
-    __syncthreads();
-    if (p == 0 && present) {
-#pragma unroll
-      for (int e = 0; e < kEach; ++e)
-        if (key[e] < in.vocab) present[key[e]] = 1;
-    }
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      rank[e] = wave_rank(key[e] >> (p * bits) & (digits - 1), bits, first + e * 64 < n, counter[wave]);
-      __builtin_amdgcn_sched_barrier(0);                     // (side by side they take more registers than there are)
-    }
-    __syncthreads();
-    uint32_t total = 0;
-    if ((int)threadIdx.x < digits)
-      for (int w = 0; w < kSortWaves; ++w) total += counter[w][threadIdx.x];
-    const uint32_t before = scan_digits(total, wave_sum);
-    if ((int)threadIdx.x < digits) base[threadIdx.x] = before;
-    __syncthreads();
-    places_of_waves(counter, base, digits);
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < kEach; ++e)
-      if (first + e * 64 < n) {
-        const uint32_t to = counter[wave][key[e] >> (p * bits) & (digits - 1)] + rank[e];
-        held[to] = key[e];
-        held_at[to] = (uint16_t)at[e];
-      }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < kEach; ++e)
-      if (first + e * 64 < n) {
-        key[e] = held[first + e * 64];
-        at[e] = held_at[first + e * 64];
-      }
+  for (int k = 0; k < kRankKeys / kRankThreads; ++k) {
+    const int i = k * kRankThreads + (int)threadIdx.x;
+    loaded[k] = i < n ? (uint32_t)(i < rows ? in.ids[i] : -1) : 0;
   }
 #pragma unroll
-  for (int e = 0; e < kEach; ++e)
-    if (first + e * 64 < n) {
-      keys[first + e * 64] = key[e];
-      positions[first + e * 64] = at[e];
+  for (int k = 0; k < kRankKeys / kRankThreads; ++k) {
+    const int i = k * kRankThreads + (int)threadIdx.x;
+    if (i < padded) held[i] = i < n ? min(loaded[k], in.vocab) << kRankBits | (uint32_t)i : 0xffffffffu;
+  }
+  if (present)
+    for (uint32_t i = threadIdx.x; i < share / 4; i += kRankThreads) ((uint32_t*)mark)[i] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *cleared = 0;
+  __syncthreads();
+  const uint32_t first_token = blockIdx.x * share;
+  if (present)
+    for (int i = threadIdx.x; i < n; i += kRankThreads) {
+      const uint32_t token = held[i] >> kRankBits;
+      if (token >= first_token && token - first_token < share) mark[token - first_token] = 1;
     }
+  const int lane = threadIdx.x & 63, first = (int)(blockIdx.x * kRankThreads + threadIdx.x) / 64 * kRankWave;
+  if (first < n) {
+    uint32_t mine[kRankWave], smaller[kRankWave] = {};
+#pragma unroll
+    for (int k = 0; k < kRankWave; ++k) mine[k] = (uint32_t)__builtin_amdgcn_readfirstlane((int)held[min(first + k, n - 1)]);
+    uint4 next = *(const uint4*)(held + 4 * lane);
+    for (int i = 256; i <= padded; i += 256) {
+      const uint4 other = next;
+      next = *(const uint4*)(held + (min(i, padded - 256) + 4 * lane));
+#pragma unroll
+      for (int k = 0; k < kRankWave; ++k)                     // (counted by the scalar unit, beside the next comparison)
+        smaller[k] += (uint32_t)(__popcll(__ballot(other.x < mine[k])) + __popcll(__ballot(other.y < mine[k])) +
+                                 __popcll(__ballot(other.z < mine[k])) + __popcll(__ballot(other.w < mine[k])));
+    }
+    if (lane < kRankWave && first + lane < n) {
+      uint32_t key = mine[0], to = smaller[0];
+#pragma unroll
+      for (int k = 1; k < kRankWave; ++k)
+        if (lane == k) {
+          key = mine[k];
+          to = smaller[k];
+        }
+      keys[to] = key >> kRankBits;
+      positions[to] = key & (kRankKeys - 1);
+    }
+  }
+  __syncthreads();
+  if (present)
+    for (uint32_t i = 16 * threadIdx.x; i < share && first_token + i < in.vocab; i += 16 * kRankThreads)
+      *(uint4*)(present + first_token + i) = *(const uint4*)(mark + i);
 }
 
 // A pass over more: each workgroup has the keys [its number x each, ...), `each` a multiple of 1,024.  First their counts.
@@ -170,6 +174,11 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(TokenKeys in
   __shared__ uint32_t counter[kSortWaves][kDigits];
   __shared__ uint32_t base[kDigits], wave_sum[kSortWaves];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, digits = 1 << bits;
+  const int64_t begin = blockIdx.x * each, end = min(in.n, begin + each);
+  const int64_t rows = kFirst ? in.rows() : 0;
+  const auto key_at = [&](int64_t t) { return t >= end ? 0 : kFirst ? in.key(t, rows) : keys_in[t]; };
+  const auto position_at = [&](int64_t t) { return t >= end ? 0 : kFirst ? (uint32_t)t : positions_in[t]; };
+  uint32_t key = key_at(begin + threadIdx.x), at = position_at(begin + threadIdx.x);     // (beside the counts, not after them)
   // The counts of all workgroups, by as many threads for a digit as there are.
   const int digit = threadIdx.x & (digits - 1), share = threadIdx.x >> bits, shares = kSortThreads >> bits;
   uint32_t all = 0, before_me = 0;
@@ -195,13 +204,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(TokenKeys in
     }
   const uint32_t before = scan_digits(total, wave_sum);       // (synchronises)
   if ((int)threadIdx.x < digits) base[threadIdx.x] = before + earlier;
-  const int64_t begin = blockIdx.x * each, end = min(in.n, begin + each);
-  const int64_t rows = kFirst ? in.rows() : 0;
   for (int64_t t0 = begin; t0 < end; t0 += kSortThreads) {
     for (int d = lane; d < digits; d += 64) counter[wave][d] = 0;
     const int64_t t = t0 + threadIdx.x;
-    const uint32_t key = kFirst ? in.key(t, rows) : t < end ? keys_in[t] : 0;
-    const uint32_t at = kFirst ? (uint32_t)t : t < end ? positions_in[t] : 0;
+    if (t0 > begin) {
+      key = key_at(t);
+      at = position_at(t);
+    }
     const uint32_t rank = wave_rank(key >> shift & (digits - 1), bits, t < end, counter[wave]);
     __syncthreads();
     places_of_waves(counter, base, digits);

@@ -99,7 +99,8 @@ def grad_want(grad, ids, vocab, scale):
 @pytest.mark.parametrize("kind,n,vocab,dim", [("even", 1, 1, 1), ("even", 1, 40, 9), ("skewed", 63, 5, 65), ("one", 64, 3, 8), ("one", 5000, 7, 130),
                                               ("skewed", 2003, 1256, 387), ("none", 300, 20, 12), ("skewed", 9001, 33000, 40),
                                               ("even", 20000, 300, 136), ("skewed", 40000, 100260, 17), ("padded", 4097, 513, 512),
-                                              ("even", 500, 12, 5000)])
+                                              ("even", 500, 12, 5000), ("skewed", 8192, 524287, 3), ("even", 500, 600000, 3), ("skewed", 8193, 511, 33),
+                                              ("skewed", 300000, 3000, 5), ("one", 270000, 2, 9)])
 def test_gradient(dtype, into, kind, n, vocab, dim):
     import paper_2507_11941_amd as bpe
 
