@@ -10,13 +10,13 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbpe_hip.so")
 SOURCES = [os.path.join(CSRC, "bpe.hip")]                       # the encoder
-OPERATOR_SOURCES = [os.path.join(CSRC, "ops.hip")]              # the operators on token batches
+OPERATOR_SOURCES = [os.path.join(CSRC, "ops", "ops.hip")]       # the operators on token batches
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 
 def headers():
     """Every header the library is compiled from: a change to any of them makes the built library stale."""
-    return sorted(glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(INCLUDE, "*.h")))
+    return sorted(glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "ops", "*.h")) + glob.glob(os.path.join(INCLUDE, "*.h")))
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",

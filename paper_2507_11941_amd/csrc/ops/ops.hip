@@ -5,7 +5,7 @@
 #include <cmath>
 #include <cstddef>
 
-#include "../../include/bpe_ops.h"
+#include "../../../include/bpe_ops.h"
 #include "embed_kernels.h"
 #include "logits_kernels.h"
 
