@@ -33,6 +33,8 @@ enum { BPE_F32 = 0, BPE_BF16 = 1, BPE_F16 = 2 };
 /* Ids and rows, 0 <= n <= BPE_MAX_TOKENS; columns, 1 <= vocab, dim <= BPE_MAX_COLUMNS.  (Their products may pass 2^32.) */
 #define BPE_MAX_TOKENS 0x3fffffff
 #define BPE_MAX_COLUMNS 0x1fffffff
+/* Strings of the losses: 0 <= batch <= BPE_MAX_STRINGS. */
+#define BPE_MAX_STRINGS 0xffffff
 
 /* out[t] = scale * weight[ids[t]], t < n.  An id outside [0, vocab) -- padding -- gives a row of zeros.
  *   weight  [vocab][dim] of `dtype`;  out [n][dim] of the same type, not overlapping weight.

@@ -83,15 +83,16 @@ LogitsWorkspace logits_layout(int64_t n, int64_t vocab, int32_t batch) {
   return w;
 }
 
-// Launches of up to `most` workgroups over n rows, `each` a row: f(first row, rows).
+// Launches over n rows, `each` workgroups a row, of no more workgroups than a grid may have: f(first row, rows).
 template <typename F>
 void for_rows(int64_t n, int64_t each, F&& f) {
   const int64_t rows = std::max<int64_t>(1, ((int64_t)1 << 21) / each);
   for (int64_t first = 0; first < n; first += rows) f(first, std::min(rows, n - first));
 }
 
-// Whether so few rows or waves that each should do little.
-constexpr int64_t kFewWaves = 2048;                         // two for each SIMD
+// A wave of the lookup copies 4 KiB of a row where that makes at least this many waves, else 1 KiB.  Rows of 8 KiB, 1 KiB and 4
+// KiB a wave: 32 rows 6.8 and 8.8 us, 2,048 9.6 and 10.1, 8,192 27.8 and 28.3, 40,961 115 and 108; 40,961 rows of 4 KiB 62.6 and 58.3.
+constexpr int64_t kManyCopies = 32768;
 
 template <typename T>
 void launch_embed(const T* weight, int64_t vocab, int64_t dim, int64_t weight_stride, const int32_t* ids, int64_t n,
@@ -103,7 +104,7 @@ void launch_embed(const T* weight, int64_t vocab, int64_t dim, int64_t weight_st
                          (unsigned)parts, count, scale, out, out_stride);
     });
   };
-  if (n * ((dim + 256 * Vec<T>::kWidth - 1) / (256 * Vec<T>::kWidth)) >= kFewWaves) launch(embed_kernel<T, 4>, 4);
+  if (n * ((dim + 256 * Vec<T>::kWidth - 1) / (256 * Vec<T>::kWidth)) >= kManyCopies) launch(embed_kernel<T, 4>, 4);
   else launch(embed_kernel<T, 1>, 1);
 }
 
@@ -116,10 +117,13 @@ struct EmbedWorkspace {
 
 EmbedWorkspace embed_layout(int64_t n, int64_t vocab, int64_t dim) {
   EmbedWorkspace w{};
-  // A chunk's rows are summed by one wave: fewer of them where there would be too few waves.
+  // A chunk's rows are summed by one wave: fewer of them where there would be too few waves, more where runs would be cut into
+  // more pieces than that needs.  Chunks of 8, 16 and 32: 2,003 rows of 2,048 columns 23.2, 26.0, 32.8 us, 8,192 37.6, 37.4, 41.7,
+  // 30,000 71.2, 65.2, 63.0, 65,536 126, 103, 95; of 387 columns 8,192 34.7, 38.8, 48.6, 30,000 49.7, 45.6, 45.9.
+  constexpr int64_t kEnoughWaves = 1536;
   const int64_t tiles = (dim + 511) / 512;
   w.chunk = kChunk;
-  while (w.chunk > 8 && (n + w.chunk - 1) / w.chunk * tiles < kFewWaves) w.chunk /= 2;
+  while (w.chunk > 8 && (n + w.chunk - 1) / w.chunk * tiles < kEnoughWaves) w.chunk /= 2;
   w.chunks = (n + w.chunk - 1) / w.chunk;
   for (int i = 0; i < 2; ++i) {
     w.keys[i] = place(w.total, (size_t)n * 4);
@@ -174,8 +178,8 @@ void launch_embed_grad(const T* grad, O* out, GradArgs a, hipStream_t stream) {
                        first, summing);
   const int64_t long_runs = a.n / (a.chunk + 1);            // at most
   if (long_runs > 0)
-    hipLaunchKernelGGL((embed_grad_join_kernel<T, O>), dim3((unsigned)std::min<int64_t>(kFewWaves, long_runs * a.tiles)), dim3(256), 0, stream,
-                       out, a);
+    hipLaunchKernelGGL((embed_grad_join_kernel<T, O>), dim3((unsigned)std::min<int64_t>(2048, long_runs * a.tiles)), dim3(256), 0, stream, out,
+                       a);
 }
 
 template <typename T>
@@ -191,7 +195,8 @@ void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, 
         hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, stream, logits, vocab, stride, first, a);
       };
       // The more threads a row has, the less of the chip is idle when the last rows end, and the more of a short row's time
-      // goes into joining them.  8,191 rows of 200 KB with 256, 512, 1,024 threads: 277, 273, 263 us; of 64 KB 92.7, 89.5, 91.4.
+      // goes into joining them.  8,191 rows of 200 KB with 256, 512, 1,024 threads: 277, 273, 263 us; of 129 KB 176, 173, 167; of
+      // 64 KB 92.7, 89.5, 91.4; of 2.5 KB 19.6, 33.9, 67.7, with 64 threads 10.8.
       if (steps >= 24) launch(logprobs_kernel<T, 1024>, 1024);
       else if (steps >= 4) launch(logprobs_kernel<T, 512>, 512);
       else if (steps >= 2) launch(logprobs_kernel<T, 256>, 256);
@@ -206,18 +211,19 @@ void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, 
 
 template <typename T, int kKind>
 void launch_rows(const T* logits, int64_t n, int64_t vocab, int64_t stride, const RowArgs& a, T* grad, hipStream_t stream) {
-  // The smallest variant whose registers hold a row: threads x vectors a lane.
+  // The smallest variant whose registers hold a row: threads x vectors a lane.  (25 vectors are what 128 registers have room for,
+  // and with 128 two workgroups of 512 threads share a compute unit, the one loading while the other stores.)
   const int64_t vecs = vocab / Vec<T>::kWidth;
   for_rows(n, 1, [&](int64_t first, int64_t rows) {
     const auto launch = [&](auto kernel, int threads) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, stream, logits, vocab, stride, first, a, grad);
     };
-    if (vecs <= 64 * 8) launch(row_kernel<T, kKind, 64, 8, 4>, 64);
-    else if (vecs <= 256 * 8) launch(row_kernel<T, kKind, 256, 8, 4>, 256);
-    else if (vecs <= 256 * 16) launch(row_kernel<T, kKind, 256, 16, 4>, 256);
-    else if (vecs <= 512 * 16) launch(row_kernel<T, kKind, 512, 16, 4>, 512);
-    else if (vecs <= 512 * 25) launch(row_kernel<T, kKind, 512, 25, 4>, 512);
-    else if (vecs <= 1024 * 25) launch(row_kernel<T, kKind, 1024, 25, 4>, 1024);
+    if (vecs <= 64 * 8) launch(row_kernel<T, kKind, 64, 8>, 64);
+    else if (vecs <= 256 * 8) launch(row_kernel<T, kKind, 256, 8>, 256);
+    else if (vecs <= 256 * 16) launch(row_kernel<T, kKind, 256, 16>, 256);
+    else if (vecs <= 512 * 16) launch(row_kernel<T, kKind, 512, 16>, 512);
+    else if (vecs <= 512 * 25) launch(row_kernel<T, kKind, 512, 25>, 512);
+    else if (vecs <= 1024 * 25) launch(row_kernel<T, kKind, 1024, 25>, 1024);
     else launch(long_row_kernel<T, kKind>, 1024);
   });
 }
@@ -307,7 +313,7 @@ int bpe_next_tokens(const int32_t* ids, int64_t n, const int64_t* offsets, int32
 }
 
 size_t bpe_loss_workspace_bytes(int64_t n, int64_t vocab, int32_t batch) {
-  if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS || batch < 0) return 0;
+  if (!is_count(n) || vocab < 1 || vocab > BPE_MAX_COLUMNS || batch < 0 || batch > BPE_MAX_STRINGS) return 0;
   return logits_layout(n, vocab, batch).total;
 }
 
@@ -372,7 +378,7 @@ int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab,
                         float scale, float* loss, float* margins, float* logprobs, void* grad, int64_t grad_stride,
                         void* workspace, size_t workspace_bytes, void* stream_ptr) {
   if (!is_count(n) || !is_matrix(logits, dtype, n, vocab, stride) || !is_matrix(grad, dtype, n, vocab, grad_stride) ||
-      batch < 0 || batch % 2 || !fits(targets, n, 4) || !offsets || !aligned(offsets, 8) || !aligned(reference, 4) ||
+      batch < 0 || batch > BPE_MAX_STRINGS || batch % 2 || !fits(targets, n, 4) || !offsets || !aligned(offsets, 8) || !aligned(reference, 4) ||
       !std::isfinite(beta) || !(smoothing >= 0.0f && smoothing <= 1.0f) || !std::isfinite(scale) || !loss || !aligned(loss, 4) ||
       !aligned(margins, 4) || !aligned(logprobs, 4) ||
       !is_workspace(workspace, workspace_bytes, bpe_loss_workspace_bytes(n, vocab, batch)))
@@ -408,7 +414,7 @@ int bpe_policy_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int
                     int by_string, float scale, float* loss, float* logprobs, void* grad, int64_t grad_stride,
                     void* workspace, size_t workspace_bytes, void* stream_ptr) {
   if (!is_count(n) || !is_matrix(logits, dtype, n, vocab, stride) || !is_matrix(grad, dtype, n, vocab, grad_stride) ||
-      batch < 0 || !fits(targets, n, 4) || !offsets || !aligned(offsets, 8) || !fits(old, n, 4) ||
+      batch < 0 || batch > BPE_MAX_STRINGS || !fits(targets, n, 4) || !offsets || !aligned(offsets, 8) || !fits(old, n, 4) ||
       !fits(advantages, advantage_by_string ? batch : n, 4) || !aligned(reference, 4) || !(clip_low >= 0.0f && clip_low <= 1.0f) ||
       !(clip_high >= 0.0f && std::isfinite(clip_high)) || !(kl_weight >= 0.0f && std::isfinite(kl_weight)) || !std::isfinite(scale) ||
       !loss || !aligned(loss, 4) || !aligned(logprobs, 4) ||

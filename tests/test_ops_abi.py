@@ -65,12 +65,12 @@ def test_loss_arguments():
     nan, inf = float("nan"), float("inf")
     call("preference_loss", dict(LOGITS, offsets=A, batch=2, reference=None, beta=0.1, smoothing=0.0, scale=1.0, loss=A, margins=None,
                                  logprobs=None, grad=A, grad_stride=7, **WORK),
-         [*BAD_LOGITS, ("offsets", None), ("offsets", A + 4), ("batch", -2), ("batch", 3), ("reference", A + 1), ("beta", nan), ("beta", inf),
+         [*BAD_LOGITS, ("offsets", None), ("offsets", A + 4), ("batch", -2), ("batch", 3), ("batch", 1 << 24), ("reference", A + 1), ("beta", nan), ("beta", inf),
           ("smoothing", -0.1), ("smoothing", 1.1), ("smoothing", nan), ("scale", nan), ("loss", None), ("margins", A + 1), ("logprobs", A + 1),
           *BAD_GRAD, *BAD_WORK])
     call("policy_loss", dict(LOGITS, offsets=A, batch=2, old=A, advantages=A, advantage_by_string=0, reference=None, low=0.2, high=0.2, kl=0.0,
                              by_string=0, scale=1.0, loss=A, logprobs=None, grad=A, grad_stride=7, **WORK),
-         [*BAD_LOGITS, ("offsets", None), ("batch", -1), ("old", None), ("advantages", None), ("reference", A + 1), ("low", -0.1), ("low", 1.1),
+         [*BAD_LOGITS, ("offsets", None), ("batch", -1), ("batch", 1 << 24), ("old", None), ("advantages", None), ("reference", A + 1), ("low", -0.1), ("low", 1.1),
           ("low", nan), ("high", -0.1), ("high", inf), ("kl", -1.0), ("kl", nan), ("scale", inf), ("loss", None), ("loss", A + 2), *BAD_GRAD,
           *BAD_WORK])
 
