@@ -128,27 +128,46 @@ __device__ inline void store_columns(O* row, const Columns& c, const float (&sum
   }
 }
 
-constexpr int kZeroRows = 16;                                // rows of the vocabulary that a wave looks for and clears
+constexpr int kClear = 1024;                                 // vectors of a workgroup that clears
 
-// Waves below `summing` sum a chunk in a tile of the columns, eight rows in flight; the others clear rows that no id names.
+// Clears what there is of rows that no id names in one stretch of the matrix, whose last vector of a row may be a part of one.
+// Workgroups that follow each other have stretches that do, 16 KiB each, as memory likes it best: 821 MB took 125 to 129 us for
+// rows of 0.5, 2 and 8 KiB, with 4, 8 or 32 KiB each 150 to 170, with whole rows for a wave 118 to 150, with some rows each 150 to 180.
+template <typename O>
+__device__ inline void clear_stretch(O* out, const GradArgs& a, int64_t stretch) {
+  constexpr int kOut = Vec<O>::kWidth;
+  const uint32_t row_vecs = (uint32_t)((a.dim + kOut - 1) / kOut);
+  const int64_t first_row = stretch * kClear / row_vecs;
+  const uint32_t first = (uint32_t)(stretch * kClear - first_row * row_vecs);
+  int64_t row[kClear / 256], column[kClear / 256];
+  bool absent[kClear / 256];
+#pragma unroll
+  for (int k = 0; k < kClear / 256; ++k) {                   // (asked for side by side)
+    const uint32_t at = first + k * 256 + threadIdx.x;
+    row[k] = first_row + at / row_vecs;
+    column[k] = (int64_t)(at % row_vecs) * kOut;
+    absent[k] = row[k] < a.vocab;
+    if (a.n > 0) absent[k] = !a.present[min(row[k], (int64_t)a.vocab - 1)] && absent[k];
+  }
+#pragma unroll
+  for (int k = 0; k < kClear / 256; ++k) {
+    if (!absent[k]) continue;
+    O* to = out + row[k] * a.out_stride + column[k];
+    if (column[k] + kOut <= a.dim)
+      Vec<O>::all(0.0f).store(to);
+    else
+      for (int i = 0; i < (int)(a.dim - column[k]); ++i) to[i] = from_float<O>(0.0f);
+  }
+}
+
+// The first `summing` workgroups sum, a wave a chunk in a tile of the columns, eight rows in flight; the others clear.
 template <typename T, typename O>
 __global__ void __launch_bounds__(256) embed_grad_kernel(const T* grad, O* out, GradArgs a, int64_t first, int64_t summing) {
   constexpr int kWidth = Vec<T>::kWidth, kDeep = 8;
-  const int64_t wave = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t group = first + blockIdx.x;
+  if (group >= summing) return clear_stretch(out, a, group - summing);
+  const int64_t wave = group * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (wave >= summing) {
-    const int64_t v0 = (wave - summing) * kZeroRows;
-    if (a.accumulate || v0 >= a.vocab) return;
-    uint64_t rows = __ballot(lane < kZeroRows && v0 + lane < a.vocab && (a.n == 0 || !a.present[v0 + lane]));
-    constexpr int kOut = Vec<O>::kWidth;
-    const int64_t whole = a.dim / kOut;
-    for (; rows; rows &= rows - 1) {
-      O* row = out + (v0 + __ffsll((unsigned long long)rows) - 1) * a.out_stride;
-      for (int64_t j = lane; j < whole; j += 64) Vec<O>::all(0.0f).store(row + j * kOut);
-      if (whole * kOut + lane < a.dim) row[whole * kOut + lane] = from_float<O>(0.0f);
-    }
-    return;
-  }
   const int64_t c = wave / a.tiles, tile = wave % a.tiles, begin = c * a.chunk;
   if (begin >= a.n) return;
   const int size = (int)min((int64_t)a.chunk, a.n - begin);

@@ -172,10 +172,11 @@ template <typename T, typename O>
 void launch_embed_grad(const T* grad, O* out, GradArgs a, hipStream_t stream) {
   constexpr int64_t kMost = (int64_t)1 << 22;               // workgroups of a launch
   a.tiles = (unsigned)((a.dim + 64 * Vec<T>::kWidth - 1) / (64 * Vec<T>::kWidth));
-  const int64_t summing = a.chunks * a.tiles, waves = summing + (a.accumulate ? 0 : (a.vocab + kZeroRows - 1) / kZeroRows);
-  for (int64_t first = 0; first < waves; first += 4 * kMost)
-    hipLaunchKernelGGL((embed_grad_kernel<T, O>), dim3(blocks(std::min(4 * kMost, waves - first), 4)), dim3(256), 0, stream, grad, out, a,
-                       first, summing);
+  const int64_t summing = (a.chunks * a.tiles + 3) / 4, row_vecs = (a.dim + Vec<O>::kWidth - 1) / Vec<O>::kWidth;
+  const int64_t groups = summing + (a.accumulate ? 0 : ((int64_t)a.vocab * row_vecs + kClear - 1) / kClear);
+  for (int64_t first = 0; first < groups; first += kMost)
+    hipLaunchKernelGGL((embed_grad_kernel<T, O>), dim3((unsigned)std::min(kMost, groups - first)), dim3(256), 0, stream, grad, out, a, first,
+                       summing);
   const int64_t long_runs = a.n / (a.chunk + 1);            // at most
   if (long_runs > 0)
     hipLaunchKernelGGL((embed_grad_join_kernel<T, O>), dim3((unsigned)std::min<int64_t>(2048, long_runs * a.tiles)), dim3(256), 0, stream, out,
