@@ -497,45 +497,62 @@ __global__ void __launch_bounds__(1024) sum_kernel(const double* values, int64_t
 }
 
 constexpr int kWeightWaves = 4;                              // strings of a workgroup
-constexpr int kShortString = 512;                            // positions that one wave goes over
+constexpr int kShortString = 1024;                           // positions that one wave goes over
 
 // The weight of each scored position in its string's loss and its advantage; and the number of scored positions of this
 // workgroup's strings.  A wave has a string, the whole workgroup one after the other those that are long.  The last workgroup:
-// rows outside every string.
+// rows outside every string.  4 us for short strings, 8 for some of hundreds of positions: reads that
+// wait for each other.
 __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(const int32_t* targets, int64_t n, int64_t vocab,
                                                                     const int64_t* offsets, int32_t batch, int by_string,
                                                                     const float* advantages, int advantage_by_string, float* weight,
                                                                     float* advantage, int32_t* scored) {
-  constexpr int kThreads = 64 * kWeightWaves;
+  constexpr int kThreads = 64 * kWeightWaves, kEach = kShortString / 64;
   if (blockIdx.x == gridDim.x - 1) return rows_outside<kThreads>(offsets, batch, n, [&](int64_t t) { weight[t] = 0.0f; });
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const auto weight_of = [&](int32_t count) { return by_string ? 1.0f / ((float)batch * (float)max(count, 1)) : 1.0f; };
   int32_t all = 0;                                           // of the waves' strings, in lane 0 of each; of long ones in thread 0
-  const auto fill = [&](int32_t i, int64_t begin, int64_t end, int at, int step, auto&& total) {
-    int32_t count = 0;
-#pragma unroll 4
-    for (int64_t t = begin + at; t < end; t += step) count += is_scored(targets, t, vocab);
-    count = total(count);
-    const float w = by_string ? (float)(1.0 / ((double)batch * max(count, 1))) : 1.0f;
-#pragma unroll 4
-    for (int64_t t = begin + at; t < end; t += step) {
-      const bool is = is_scored(targets, t, vocab);
-      weight[t] = is ? w : 0.0f;
-      if (is) advantage[t] = advantages[advantage_by_string ? i : t];
-    }
-    if (at == 0) all += count;
-  };
   for (int32_t i0 = blockIdx.x * kWeightWaves; i0 < batch; i0 += (gridDim.x - 1) * kWeightWaves) {
     const int32_t i = i0 + wave;
     int64_t begin = 0, end = 0;
     if (i < batch) string_rows(offsets, i, n, &begin, &end);
-    if (end - begin <= kShortString)
-      fill(i, begin, end, lane, 64, [](int32_t c) {
-        for (int d = 32; d >= 1; d >>= 1) c += __shfl_xor(c, d);
-        return c;
-      });
+    if (end - begin <= kShortString) {
+      bool is[kEach];
+      float adv[kEach];
+      int32_t count = 0;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {                      // (all reads side by side)
+        const int64_t t = begin + k * 64 + lane;
+        is[k] = t < end && is_scored(targets, t, vocab);
+        adv[k] = t < end ? advantages[advantage_by_string ? i : t] : 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) count += __popcll(__ballot(is[k]));
+      const float w = weight_of(count);
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        const int64_t t = begin + k * 64 + lane;
+        if (t >= end) continue;
+        weight[t] = is[k] ? w : 0.0f;
+        advantage[t] = adv[k];
+      }
+      if (lane == 0) all += count;
+    }
+    if (!__syncthreads_or(end - begin > kShortString)) continue;
     for (int32_t j = i0; j < min(i0 + kWeightWaves, batch); ++j) {
       string_rows(offsets, j, n, &begin, &end);
-      if (end - begin > kShortString) fill(j, begin, end, threadIdx.x, kThreads, [](int32_t c) { return sum_workgroup<kThreads>(c); });
+      if (end - begin <= kShortString) continue;
+      int32_t count = 0;
+#pragma unroll 4
+      for (int64_t t = begin + threadIdx.x; t < end; t += kThreads) count += is_scored(targets, t, vocab);
+      count = sum_workgroup<kThreads>(count);
+      const float w = weight_of(count);
+#pragma unroll 4
+      for (int64_t t = begin + threadIdx.x; t < end; t += kThreads) {
+        weight[t] = is_scored(targets, t, vocab) ? w : 0.0f;
+        advantage[t] = advantages[advantage_by_string ? j : t];
+      }
+      if (threadIdx.x == 0) all += count;
     }
   }
   all = sum_workgroup<kThreads>(lane == 0 ? all : 0);

@@ -187,3 +187,15 @@ def test_refusals():
         with pytest.raises(ValueError):
             bad()
     torch.cuda.synchronize()
+
+
+def test_more_rows_than_one_launch_takes():
+    import paper_2507_11941_amd as bpe
+
+    n, vocab, dim = (1 << 21) + 1003, 700, 3
+    weight, ids = matrix(vocab, dim, torch.float32, 1), some_ids("skewed", n, vocab, 2)
+    want = embed_want(weight, ids, 2.0)
+    assert torch.equal(bpe.embed_tokens(weight, ids.to(dev()), 2.0).cpu().double(), want)
+    grad = matrix(n, dim, torch.float32, 3)
+    got = bpe.embed_tokens_grad(grad, ids.to(dev()), vocab, 1.0)
+    assert_near(got, *grad_want(grad, ids, vocab, 1.0), "gradient")

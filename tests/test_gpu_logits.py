@@ -248,3 +248,9 @@ def test_refusals():
         with pytest.raises(ValueError):
             bad()
     torch.cuda.synchronize()
+
+
+def test_more_rows_than_one_launch_takes():
+    """Rows are launched 2^21 at a time (and parts of rows as many): those of the second launch are where they belong."""
+    n, vocab = (1 << 21) + 1003, 5
+    check_all(some_logits(n, vocab, torch.float16, 4), some_targets(n, vocab, 5), some_upstream(n, 6))

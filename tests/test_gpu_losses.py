@@ -108,7 +108,7 @@ def test_preference_of_far_apart_strings():
         assert torch.isfinite(grad).all() and bool(grad.any()) == (turn > 0)
 
 
-POLICIES = [[5], [3, 4, 0, 1], [0, 0], [64, 300, 1, 2, 700], [900]]
+POLICIES = [[5], [3, 4, 0, 1], [0, 0], [64, 300, 1, 2, 700], [900], [1500, 3, 0, 1100, 1024]]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
