@@ -1,8 +1,8 @@
 """ctypes binding of include/bpe_ops.h, the operators on token batches: argument marshalling only.
 
 Every function enqueues on ``stream`` (default: torch's current stream of the tensors' device) and synchronises nothing.
-Outputs and workspaces that are not given are allocated.  Matrices may have any stride between rows, but not between columns;
-vectors are contiguous.  What the kernels cannot take is refused (ValueError), never copied into shape."""
+Outputs and workspaces that are not given are allocated, on that stream.  Matrices may have any stride between rows, but not
+between columns; vectors are contiguous.  What the kernels cannot take is refused (ValueError), never copied into shape."""
 from __future__ import annotations
 
 import ctypes
@@ -67,22 +67,34 @@ def _vector(t, what, dev, dtype, count):
     return t.data_ptr()
 
 
-def _enqueue(name, dev, stream, tensors, call):
-    """call(stream handle), on the tensors' device; tensors that do not belong to `stream` are kept until it is done with them.
-    (The handle without a Stream object, and the device without the check that torch has begun: 2 us of a small call's 11.)"""
+def _enqueue(function, dev, *args):
+    """function(*args, handle of the device's current stream).  (The handle without a Stream object, and the device without the
+    check that torch has begun: 2 us of a small call's 11.)"""
     if dev.index != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
-            return _enqueue(name, dev, stream, tensors, call)
-    if stream is None:
-        code = call(torch._C._cuda_getCurrentRawStream(dev.index))
-    else:
-        if stream != torch.cuda.current_stream(dev):
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(stream)
-        code = call(stream.cuda_stream)
+            return _enqueue(function, dev, *args)
+    code = function(*args, torch._C._cuda_getCurrentRawStream(dev.index))
     if code != 0:
-        _check(code, "bpe_" + name)
+        _check(code, function.__name__)
+
+
+def _on(stream, function, *args):
+    """function(*args) on `stream`.  What it allocates belongs to that stream: a block of the caller's could still be in use by
+    work that the caller's stream has queued.  No tensor's memory is given away before both streams are done with it."""
+    _load()
+    if args[0].device != stream.device:
+        raise ValueError(f"stream is of {stream.device}, not {args[0].device}")
+    caller = torch.cuda.current_stream(stream.device)
+    if stream == caller:
+        return function(*args)
+    with torch.cuda.stream(stream):
+        results = function(*args)
+    for t in args:
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
+    for t in results if isinstance(results, tuple) else (results,):
+        t.record_stream(caller)
+    return results
 
 
 def _strings(offsets, dev):
@@ -117,17 +129,18 @@ def embed_tokens(weight, ids, scale: float = 1.0, count=None, out=None, stream=N
     """``out[t] = scale * weight[ids[t]]``: rows of an embedding [vocab, dim] for int32 ids [n]; zeros for an id outside the
     vocabulary (padding).  ``count``: one int64 on the GPU, from which row on ids and out are left alone (``out_offsets[-1:]``
     of an encoded batch, whose ids need not all be in use)."""
+    if stream is not None:
+        return _on(stream, embed_tokens, weight, ids, scale, count, out)
     lib = _lib or _load()
     stride, dev = _matrix(weight, "weight"), weight.device
     n, dim = ids.numel(), weight.shape[1]
     ids_ptr = _vector(ids, "ids", dev, torch.int32, None)
     if out is None:
-        out = weight.new_empty((n, dim))
-    out_stride = _matrix(out, "out", dev, (n, dim), weight.dtype)
-    count_ptr = _count(count, dev)
-    _enqueue("embed_tokens", dev, stream, (weight, ids, count, out), lambda s: lib.bpe_embed_tokens(
-        weight.data_ptr(), _TYPES[weight.dtype], weight.shape[0], dim, stride, ids_ptr, n, count_ptr, scale, out.data_ptr(),
-        out_stride, s))
+        out, out_stride = weight.new_empty((n, dim)), dim
+    else:
+        out_stride = _matrix(out, "out", dev, (n, dim), weight.dtype)
+    _enqueue(lib.bpe_embed_tokens, dev, weight.data_ptr(), _TYPES[weight.dtype], weight.shape[0], dim, stride, ids_ptr, n,
+             None if count is None else _count(count, dev), scale, out.data_ptr(), out_stride)
     return out
 
 
@@ -136,6 +149,8 @@ def embed_tokens_grad(grad, ids, vocab: int, scale: float = 1.0, count=None, out
     """The gradient [vocab, dim] of an embedding's weights from that of its output [n, dim]: row v is ``scale`` times the sum
     of grad[t] over the t with ids[t] = v.  Its type is ``out``'s or ``dtype``: float32 or grad's (the default).  With
     ``accumulate`` it is added to what ``out`` holds."""
+    if stream is not None:
+        return _on(stream, embed_tokens_grad, grad, ids, vocab, scale, count, out, dtype, accumulate, workspace)
     lib = _lib or _load()
     stride, dev = _matrix(grad, "grad"), grad.device
     n, dim = grad.shape
@@ -151,15 +166,16 @@ def embed_tokens_grad(grad, ids, vocab: int, scale: float = 1.0, count=None, out
     out_stride = _matrix(out, "out", dev, (vocab, dim))
     count_ptr = _count(count, dev)
     workspace = _workspace(workspace, lib.bpe_embed_tokens_grad_workspace_bytes(n, vocab, dim), dev, "embed_tokens_grad")
-    _enqueue("embed_tokens_grad", dev, stream, (grad, ids, count, out, workspace), lambda s: lib.bpe_embed_tokens_grad(
-        grad.data_ptr(), _TYPES[grad.dtype], stride, ids_ptr, n, count_ptr, vocab, dim, scale, 1 if accumulate else 0,
-        out.data_ptr(), _TYPES[out.dtype], out_stride, workspace.data_ptr(), workspace.numel(), s))
+    _enqueue(lib.bpe_embed_tokens_grad, dev, grad.data_ptr(), _TYPES[grad.dtype], stride, ids_ptr, n, count_ptr, vocab, dim, scale,
+             1 if accumulate else 0, out.data_ptr(), _TYPES[out.dtype], out_stride, workspace.data_ptr(), workspace.numel())
     return out
 
 
 def next_tokens(ids, offsets, first=None, out=None, stream=None):
     """What each position of a packed batch is to predict: the id after it in its string (int64 offsets [B + 1]); -1, not
     scored, at a string's end and where that id is among the string's ``first`` tokens (int32 [B]: prompts)."""
+    if stream is not None:
+        return _on(stream, next_tokens, ids, offsets, first, out)
     lib = _lib or _load()
     dev, n = ids.device, ids.numel()
     if not ids.is_cuda:
@@ -168,65 +184,67 @@ def next_tokens(ids, offsets, first=None, out=None, stream=None):
     offsets_ptr, batch = _strings(offsets, dev)
     first_ptr = None if first is None else _vector(first, "first", dev, torch.int32, batch)
     if out is None:
-        out = ids.new_empty(n)
-    out_ptr = _vector(out, "out", dev, torch.int32, n)
-    _enqueue("next_tokens", dev, stream, (ids, offsets, first, out),
-             lambda s: lib.bpe_next_tokens(ids_ptr, n, offsets_ptr, batch, first_ptr, out_ptr, s))
+        out = torch.empty_like(ids)
+    _enqueue(lib.bpe_next_tokens, dev, ids_ptr, n, offsets_ptr, batch, first_ptr, _vector(out, "out", dev, torch.int32, n))
     return out
 
 
 def _grad_of(logits, out):
+    """(the gradient's matrix, the stride between its rows)"""
     if out is None:
-        out = logits.new_empty(logits.shape)
-    stride = _matrix(out, "out", logits.device, tuple(logits.shape), logits.dtype)
-    return out, stride
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+        return out, out.shape[1]
+    return out, _matrix(out, "out", logits.device, tuple(logits.shape), logits.dtype)
 
 
 def token_logprobs(logits, targets, workspace=None, stream=None):
     """(log-probabilities float32 [n] of the int32 targets [n] under logits [n, vocab], logarithms float32 [n] of the rows'
     sums of exponentials).  Rows whose target is outside the vocabulary are not scored: not read, and 0 in both."""
+    if stream is not None:
+        return _on(stream, token_logprobs, logits, targets, workspace)
     lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
     targets_ptr = _vector(targets, "targets", dev, torch.int32, n)
-    logprobs, lse = torch.empty(n, dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
+    logprobs = torch.empty(n, dtype=torch.float32, device=dev)
+    lse = torch.empty_like(logprobs)
     need = lib.bpe_token_logprobs_workspace_bytes(n, vocab)
     workspace = _workspace(workspace, need, dev, "token_logprobs") if need else None
-    _enqueue("token_logprobs", dev, stream, (logits, targets, logprobs, lse, workspace), lambda s: lib.bpe_token_logprobs(
-        logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, logprobs.data_ptr(), lse.data_ptr(),
-        _pointer(workspace), need, s))
+    _enqueue(lib.bpe_token_logprobs, dev, logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr,
+             logprobs.data_ptr(), lse.data_ptr(), _pointer(workspace), need)
     return logprobs, lse
 
 
 def token_logprobs_grad(logits, targets, lse, upstream, out=None, stream=None):
     """The gradient [n, vocab] with respect to the logits of ``(upstream * logprobs).sum()``, from the ``lse`` that
     ``token_logprobs`` returned.  ``out`` may be ``logits`` itself."""
+    if stream is not None:
+        return _on(stream, token_logprobs_grad, logits, targets, lse, upstream, out)
     lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
     targets_ptr = _vector(targets, "targets", dev, torch.int32, n)
     lse_ptr, upstream_ptr = _vector(lse, "lse", dev, torch.float32, n), _vector(upstream, "upstream", dev, torch.float32, n)
     out, out_stride = _grad_of(logits, out)
-    _enqueue("token_logprobs_grad", dev, stream, (logits, targets, lse, upstream, out), lambda s: lib.bpe_token_logprobs_grad(
-        logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, lse_ptr, upstream_ptr, out.data_ptr(),
-        out_stride, s))
+    _enqueue(lib.bpe_token_logprobs_grad, dev, logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, lse_ptr,
+             upstream_ptr, out.data_ptr(), out_stride)
     return out
 
 
 def token_logprobs_and_grad(logits, targets, upstream, out=None, stream=None):
     """(logprobs, lse, gradient of ``(upstream * logprobs).sum()``) in one pass over the logits, for an upstream that is known
     before: of cross entropy it is -1 / (number of scored tokens).  ``out`` may be ``logits`` itself."""
+    if stream is not None:
+        return _on(stream, token_logprobs_and_grad, logits, targets, upstream, out)
     lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
     targets_ptr = _vector(targets, "targets", dev, torch.int32, n)
     upstream_ptr = _vector(upstream, "upstream", dev, torch.float32, n)
-    logprobs, lse = torch.empty(n, dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
+    logprobs, lse = torch.empty_like(upstream), torch.empty_like(upstream)
     out, out_stride = _grad_of(logits, out)
-    _enqueue("token_logprobs_and_grad", dev, stream, (logits, targets, upstream, logprobs, lse, out),
-             lambda s: lib.bpe_token_logprobs_and_grad(
-                 logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, upstream_ptr, logprobs.data_ptr(),
-                 lse.data_ptr(), out.data_ptr(), out_stride, s))
+    _enqueue(lib.bpe_token_logprobs_and_grad, dev, logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr,
+             upstream_ptr, logprobs.data_ptr(), lse.data_ptr(), out.data_ptr(), out_stride)
     return logprobs, lse, out
 
 
@@ -235,6 +253,8 @@ def preference_loss(logits, targets, offsets, reference=None, beta: float = 0.1,
     """Preference loss over pairs of strings, 2k preferred to 2k + 1: (loss, margins float32 [B / 2], logprobs float32 [n],
     ``scale`` times the gradient with respect to the logits).  ``reference``: float32 [n], the reference model's logprobs.
     ``out`` may be ``logits`` itself.  The formulas are in include/bpe_ops.h."""
+    if stream is not None:
+        return _on(stream, preference_loss, logits, targets, offsets, reference, beta, smoothing, scale, out, workspace)
     lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
@@ -247,11 +267,9 @@ def preference_loss(logits, targets, offsets, reference=None, beta: float = 0.1,
     logprobs = torch.empty(n, dtype=torch.float32, device=dev)
     out, out_stride = _grad_of(logits, out)
     workspace = _workspace(workspace, lib.bpe_loss_workspace_bytes(n, vocab, batch), dev, "logits")
-    _enqueue("preference_loss", dev, stream, (logits, targets, offsets, reference, loss, margins, logprobs, out, workspace),
-             lambda s: lib.bpe_preference_loss(
-                 logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, offsets_ptr, batch, reference_ptr,
-                 beta, smoothing, scale, loss.data_ptr(), margins.data_ptr(), logprobs.data_ptr(), out.data_ptr(), out_stride,
-                 workspace.data_ptr(), workspace.numel(), s))
+    _enqueue(lib.bpe_preference_loss, dev, logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, offsets_ptr,
+             batch, reference_ptr, beta, smoothing, scale, loss.data_ptr(), margins.data_ptr(), logprobs.data_ptr(), out.data_ptr(),
+             out_stride, workspace.data_ptr(), workspace.numel())
     return loss, margins, logprobs, out
 
 
@@ -262,6 +280,9 @@ def policy_loss(logits, targets, offsets, old, advantages, reference=None, clip_
     [n], or [B], one for all of a string (where n = B, it is by string if ``per`` is "string").  ``per``: "token", all scored
     tokens weigh the same, or "string", all strings.  ``out`` may be ``logits`` itself.  The formulas are in
     include/bpe_ops.h."""
+    if stream is not None:
+        return _on(stream, policy_loss, logits, targets, offsets, old, advantages, reference, clip_low, clip_high, kl_weight, per,
+                   scale, out, workspace)
     lib = _lib or _load()
     stride, dev = _matrix(logits, "logits"), logits.device
     n, vocab = logits.shape
@@ -274,12 +295,10 @@ def policy_loss(logits, targets, offsets, old, advantages, reference=None, clip_
     whole = advantages.numel() == batch and (batch != n or by_string)
     advantages_ptr = _vector(advantages, "advantages", dev, torch.float32, batch if whole else n)
     reference_ptr = None if reference is None else _vector(reference, "reference", dev, torch.float32, n)
-    loss, logprobs = torch.empty((), dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
+    loss, logprobs = torch.empty((), dtype=torch.float32, device=dev), torch.empty_like(old)
     out, out_stride = _grad_of(logits, out)
     workspace = _workspace(workspace, lib.bpe_loss_workspace_bytes(n, vocab, batch), dev, "logits")
-    _enqueue("policy_loss", dev, stream, (logits, targets, offsets, old, advantages, reference, loss, logprobs, out, workspace),
-             lambda s: lib.bpe_policy_loss(
-                 logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, offsets_ptr, batch, old_ptr,
-                 advantages_ptr, 1 if whole else 0, reference_ptr, clip_low, clip_high, kl_weight, 1 if by_string else 0, scale,
-                 loss.data_ptr(), logprobs.data_ptr(), out.data_ptr(), out_stride, workspace.data_ptr(), workspace.numel(), s))
+    _enqueue(lib.bpe_policy_loss, dev, logits.data_ptr(), _TYPES[logits.dtype], n, vocab, stride, targets_ptr, offsets_ptr, batch,
+             old_ptr, advantages_ptr, 1 if whole else 0, reference_ptr, clip_low, clip_high, kl_weight, 1 if by_string else 0,
+             scale, loss.data_ptr(), logprobs.data_ptr(), out.data_ptr(), out_stride, workspace.data_ptr(), workspace.numel())
     return loss, logprobs, out

@@ -199,3 +199,24 @@ def test_more_rows_than_one_launch_takes():
     grad = matrix(n, dim, torch.float32, 3)
     got = bpe.embed_tokens_grad(grad, ids.to(dev()), vocab, 1.0)
     assert_near(got, *grad_want(grad, ids, vocab, 1.0), "gradient")
+
+
+def test_outputs_belong_to_the_stream_that_writes_them():
+    """A block that the caller's stream has freed but is still writing to must not become the output of a call on another stream."""
+    import paper_2507_11941_amd as bpe
+
+    n, dim = 4096, 1024
+    weight, ids = torch.randn(1000, dim, device=dev()), torch.arange(n, dtype=torch.int32, device=dev()) % 1000
+    want = weight[ids.long()]
+    grad_want = bpe.embed_tokens_grad(want, ids, 1000)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    late = [torch.empty(n, dim, device=dev()), torch.empty(1000, dim, device=dev())]
+    torch.cuda._sleep(20_000_000)
+    for t in late:
+        t.fill_(7.0)
+    del late, t
+    got = bpe.embed_tokens(weight, ids, stream=side)
+    grad = bpe.embed_tokens_grad(got, ids, 1000, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(grad, grad_want)
