@@ -131,8 +131,8 @@ struct RowArgs {
   int64_t grad_stride;
   // kRowPolicy
   const float* weight;        // of each row's loss; 0: not scored
-  const int32_t* scored;      // null, or the numbers of scored rows whose sum the loss is divided by
-  int n_scored;
+  const int32_t* scored;      // the numbers of scored rows whose sum the loss is divided by,
+  int n_scored;               // if there are any of them
   const float* advantage;     // of each row
   const float* old;
   const float* reference;
@@ -140,32 +140,66 @@ struct RowArgs {
   double* value;              // of each row: its share of the loss
 };
 
+// What a row has besides its logits.  Everything is read before the logits, side by side: read when the row's sums are there, it
+// would be one more wait for memory while the row occupies its compute unit (policy loss of 8,000 rows of 12,000 bfloat16: 91 us
+// instead of 84; 8,190 of 100,260: 589 instead of 585).
+struct RowInputs {
+  int32_t target;
+  float weight, upstream, advantage, old, reference;
+  int32_t counted, counted_more;                            // this lane's part of the number of scored rows
+};
+
+template <int kKind>
+__device__ inline RowInputs inputs_of(const RowArgs& a, int64_t t) {
+  RowInputs in{};
+  in.target = a.targets[t];
+  in.weight = kKind == kRowPolicy ? a.weight[t] : 1.0f;
+  if constexpr (kKind == kRowStep) in.upstream = a.upstream[t];
+  if constexpr (kKind == kRowPolicy) {
+    in.advantage = a.advantage[t];
+    in.old = a.old[t];
+    if (a.reference) in.reference = a.reference[t];
+    const int lane = threadIdx.x & 63;
+    if (lane < a.n_scored) in.counted = a.scored[lane];
+    for (int i = 64 + lane; i < a.n_scored; i += 64) in.counted_more += a.scored[i];
+  }
+  return in;
+}
+
+__device__ inline bool is_scored(const RowInputs& in, int64_t vocab) {
+  return in.target >= 0 && in.target < vocab && in.weight != 0.0f;
+}
+
 // The loss of one token under the clipped policy, and its derivative with respect to the token's log-probability.
-__device__ inline float policy_value(const RowArgs& a, int64_t t, float lp, float* slope) {
-  const float advantage = a.advantage[t];
-  const float ratio = expf(lp - a.old[t]);
-  const float free = ratio * advantage, clipped = fminf(fmaxf(ratio, 1.0f - a.low), 1.0f + a.high) * advantage;
+__device__ inline float policy_value(const RowArgs& a, const RowInputs& in, float lp, float* slope) {
+  const float ratio = expf(lp - in.old);
+  const float free = ratio * in.advantage, clipped = fminf(fmaxf(ratio, 1.0f - a.low), 1.0f + a.high) * in.advantage;
   float value = -fminf(free, clipped);
   *slope = free <= clipped ? -free : 0.0f;
   if (a.reference) {
-    const float d = a.reference[t] - lp;
+    const float d = in.reference - lp;
     value += a.kl_weight * (expm1f(d) - d);
     *slope -= a.kl_weight * expm1f(d);
   }
   return value;
 }
 
-// What a row's log-probability gives besides: the outputs of thread 0, and the factor of the row's gradient.
+// What a row's log-probability gives besides, by one wave: the outputs of thread 0, and the factor of the row's gradient.
 template <int kKind>
-__device__ inline float finish_row(const RowArgs& a, int64_t t, float weight, Stats all, float lp) {
+__device__ inline float finish_row(const RowArgs& a, int64_t t, const RowInputs& in, Stats all, float lp) {
   if (threadIdx.x == 0) {
     if (a.logprobs) a.logprobs[t] = lp;
     if (a.lse) a.lse[t] = lse_of(all);
   }
-  if constexpr (kKind == kRowStep) return a.upstream[t];
+  if constexpr (kKind == kRowStep) return in.upstream;
   if constexpr (kKind == kRowPolicy) {
-    float slope;
-    const float value = policy_value(a, t, lp, &slope);
+    float weight = in.weight, slope;
+    if (a.n_scored > 0) {
+      int32_t scored = in.counted + in.counted_more;
+      for (int d = 32; d >= 1; d >>= 1) scored += __shfl_xor(scored, d);
+      weight = 1.0f / (float)scored;
+    }
+    const float value = policy_value(a, in, lp, &slope);
     if (threadIdx.x == 0) a.value[t] = (double)weight * value;
     return a.scale * weight * slope;
   }
@@ -179,20 +213,6 @@ __device__ inline void skip_row(const RowArgs& a, int64_t t) {
     if (a.lse) a.lse[t] = 0.0f;
     if (kKind == kRowPolicy) a.value[t] = 0.0;
   }
-}
-
-template <int kKind>
-__device__ inline bool scored_row(const RowArgs& a, int64_t t, int64_t vocab, int32_t* target, float* weight) {
-  *target = a.targets[t];
-  *weight = kKind == kRowPolicy ? a.weight[t] : 1.0f;
-  const bool scored = *target >= 0 && *target < vocab && *weight != 0.0f;
-  if (kKind == kRowPolicy && scored && a.scored) {
-    int32_t all = 0;
-    for (int i = threadIdx.x & 63; i < a.n_scored; i += 64) all += a.scored[i];
-    for (int d = 32; d >= 1; d >>= 1) all += __shfl_xor(all, d);
-    *weight = 1.0f / (float)__builtin_amdgcn_readfirstlane(all);
-  }
-  return scored;
 }
 
 template <typename T, int kThreads>
@@ -219,13 +239,12 @@ __device__ inline Vec<T> grad_of(const Vec<T>& v, float reference, float share) 
 template <typename T, int kThreads>
 __global__ void __launch_bounds__(kThreads) logprobs_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, RowArgs a) {
   const int64_t t = first + blockIdx.x;
-  int32_t target;
-  float weight;
-  if (!scored_row<kRowLogprob>(a, t, vocab, &target, &weight)) return skip_row<kRowLogprob>(a, t);
+  const RowInputs in = inputs_of<kRowLogprob>(a, t);
+  if (!is_scored(in, vocab)) return skip_row<kRowLogprob>(a, t);
   const T* x = logits + t * stride;
-  const float at_target = to_float(x[target]);
+  const float at_target = to_float(x[in.target]);
   const Stats all = join_workgroup<kThreads>(stream<T, kThreads>(x, 0, vocab));
-  if (threadIdx.x == 0) finish_row<kRowLogprob>(a, t, weight, all, logprob_of(at_target, all));
+  if (threadIdx.x == 0) finish_row<kRowLogprob>(a, t, in, all, logprob_of(at_target, all));
 }
 
 // Few rows: each is split among `parts` workgroups, whose statistics another kernel joins.
@@ -244,14 +263,13 @@ template <typename T>
 __global__ void __launch_bounds__(64) logprobs_join_kernel(const T* logits, int64_t vocab, int64_t stride, int parts,
                                                            const Stats* part, RowArgs a) {
   const int64_t t = blockIdx.x;
-  int32_t target;
-  float weight;
-  if (!scored_row<kRowLogprob>(a, t, vocab, &target, &weight)) return skip_row<kRowLogprob>(a, t);
-  const float at_target = to_float(logits[t * stride + target]);
+  const RowInputs in = inputs_of<kRowLogprob>(a, t);
+  if (!is_scored(in, vocab)) return skip_row<kRowLogprob>(a, t);
+  const float at_target = to_float(logits[t * stride + in.target]);
   Stats mine = {-INFINITY, 0.0f};
   for (int k = threadIdx.x; k < parts; k += 64) mine = join(mine, part[t * parts + k]);
   const Stats all = join_workgroup<64>(mine);
-  if (threadIdx.x == 0) finish_row<kRowLogprob>(a, t, weight, all, logprob_of(at_target, all));
+  if (threadIdx.x == 0) finish_row<kRowLogprob>(a, t, in, all, logprob_of(at_target, all));
 }
 
 // Log-probability and gradient of a row in one pass: the row stays in the workgroup's registers, kVecs x 16 bytes a lane, at most
@@ -262,9 +280,8 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const T* logits, int64
   __shared__ float factor[2];
   const int64_t t = first + blockIdx.x;
   T* g = grad + t * a.grad_stride;
-  int32_t target;
-  float weight;
-  if (!scored_row<kKind>(a, t, vocab, &target, &weight)) {
+  const RowInputs in = inputs_of<kKind>(a, t);
+  if (!is_scored(in, vocab)) {
     skip_row<kKind>(a, t);
     return zero_row<T, kThreads>(g, vocab);
   }
@@ -279,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const T* logits, int64
   }
   float last = -INFINITY;                                   // one of those behind the whole vectors
   if (lane_at < rest) last = to_float(x[whole * kWidth + lane_at]);
-  const float at_target = to_float(x[target]);
+  const float at_target = to_float(x[in.target]);
   Stats mine = {-INFINITY, 0.0f};
 #pragma unroll
   for (int k = 0; k + kDeep <= kVecs; k += kDeep) absorb<T, kDeep>(mine, v + k);
@@ -287,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const T* logits, int64
   const Stats all = join_workgroup<kThreads>(join(mine, {last, 1.0f}));
   if (threadIdx.x < 64) {
     const float lp = logprob_of(at_target, all);
-    const float c = finish_row<kKind>(a, t, weight, all, lp);
+    const float c = finish_row<kKind>(a, t, in, all, lp);
     if (threadIdx.x == 0) {
       factor[0] = c;
       factor[1] = -c * expm1f(lp);                          // the gradient at the target: 1 - p without the cancellation
@@ -305,8 +322,8 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const T* logits, int64
     if (k * kThreads + lane_at < whole) grad_of(v[k], all.m, share).store(g + (k * kThreads + lane_at) * kWidth);
   if (lane_at < rest) g[whole * kWidth + lane_at] = from_float<T>(share * exp_of(last, all.m));
   // The target's element once more, by the thread that has just written it.
-  if (lane_at == (target < whole * kWidth ? target / kWidth % kThreads : target - whole * kWidth))
-    g[target] = from_float<T>(factor[1]);
+  if (lane_at == (in.target < whole * kWidth ? in.target / kWidth % kThreads : in.target - whole * kWidth))
+    g[in.target] = from_float<T>(factor[1]);
 }
 
 // The same for rows that no workgroup's registers hold (over 400 KiB): they are read twice.
@@ -316,18 +333,17 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const T* logits, int64_t
   __shared__ float factor[2];
   const int64_t t = first + blockIdx.x;
   T* g = grad + t * a.grad_stride;
-  int32_t target;
-  float weight;
-  if (!scored_row<kKind>(a, t, vocab, &target, &weight)) {
+  const RowInputs in = inputs_of<kKind>(a, t);
+  if (!is_scored(in, vocab)) {
     skip_row<kKind>(a, t);
     return zero_row<T, kThreads>(g, vocab);
   }
   const T* x = logits + t * stride;
-  const float at_target = to_float(x[target]);
+  const float at_target = to_float(x[in.target]);
   const Stats all = join_workgroup<kThreads>(stream<T, kThreads>(x, 0, vocab));
   if (threadIdx.x < 64) {
     const float lp = logprob_of(at_target, all);
-    const float c = finish_row<kKind>(a, t, weight, all, lp);
+    const float c = finish_row<kKind>(a, t, in, all, lp);
     if (threadIdx.x == 0) {
       factor[0] = c;
       factor[1] = -c * expm1f(lp);                          // the gradient at the target: 1 - p without the cancellation
@@ -341,8 +357,8 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const T* logits, int64_t
   for (int64_t j = threadIdx.x; j < whole; j += kThreads) grad_of(Vec<T>::load(x + j * kWidth), all.m, share).store(g + j * kWidth);
   const int64_t j = whole * kWidth + threadIdx.x;
   if (j < vocab) g[j] = from_float<T>(share * exp_of(to_float(x[j]), all.m));
-  if (threadIdx.x == (target < whole * kWidth ? target / kWidth % kThreads : target - whole * kWidth))
-    g[target] = from_float<T>(factor[1]);
+  if (threadIdx.x == (in.target < whole * kWidth ? in.target / kWidth % kThreads : in.target - whole * kWidth))
+    g[in.target] = from_float<T>(factor[1]);
 }
 
 // The sum over a workgroup, in every thread, in a fixed order.

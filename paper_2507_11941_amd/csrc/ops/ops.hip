@@ -431,8 +431,8 @@ int bpe_policy_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int
   a.logprobs = logprobs;
   a.grad_stride = grad_stride;
   a.weight = (float*)(ws + w.upstream);
-  a.scored = by_string ? nullptr : counts;
-  a.n_scored = (int)groups;
+  a.scored = counts;
+  a.n_scored = by_string ? 0 : (int)groups;
   a.advantage = (float*)(ws + w.advantage);
   a.old = old;
   a.reference = kl_weight > 0.0f ? reference : nullptr;
