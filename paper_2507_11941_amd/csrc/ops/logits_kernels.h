@@ -378,9 +378,15 @@ __device__ inline V sum_workgroup(V mine) {
 // The sum of values, by one workgroup.
 template <int kThreads>
 __device__ inline void sum_values(const double* values, int64_t n, float* sum) {
+  constexpr int kDeep = 16;
   double mine = 0.0;
-#pragma unroll 8
-  for (int64_t i = threadIdx.x; i < n; i += kThreads) mine += values[i];
+  for (int64_t i = threadIdx.x; i < n; i += kThreads * kDeep) {
+    double v[kDeep];
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) v[k] = values[min(i + k * kThreads, n - 1)];       // (all reads side by side)
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) mine += i + k * kThreads < n ? v[k] : 0.0;
+  }
   mine = sum_workgroup<kThreads>(mine);
   if (threadIdx.x == 0) *sum = (float)mine;
 }
@@ -489,12 +495,25 @@ __global__ void __launch_bounds__(256) pair_kernel(const float* logprobs, const 
   int64_t begin, middle, end, unused;
   string_rows(offsets, 2 * k, n, &begin, &middle);
   string_rows(offsets, 2 * k + 1, n, &unused, &end);
+  constexpr int kDeep = 4;
   double sum = 0.0;
-  for (int64_t t = begin + threadIdx.x; t < end; t += 256)
-    if (is_scored(targets, t, vocab)) {
-      const double apart = (double)logprobs[t] - (reference ? (double)reference[t] : 0.0);
-      sum += t < middle ? apart : -apart;
+  for (int64_t t0 = begin + threadIdx.x; t0 < end; t0 += 256 * kDeep) {
+    int32_t target[kDeep];
+    float lp[kDeep], ref[kDeep];
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) {                        // (all reads side by side)
+      const int64_t t = min(t0 + k * 256, end - 1);
+      target[k] = targets[t];
+      lp[k] = logprobs[t];
+      ref[k] = reference ? reference[t] : 0.0f;
     }
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) {
+      const int64_t t = t0 + k * 256;
+      const double apart = (double)lp[k] - (double)ref[k];
+      if (t < end && target[k] >= 0 && target[k] < vocab) sum += t < middle ? apart : -apart;
+    }
+  }
   const double z = (double)beta * sum_workgroup<256>(sum);
   // -log sigmoid(z) = max(-z, 0) + log(1 + exp(-|z|))
   const double tail = log1p(exp(-fabs(z)));
@@ -559,8 +578,13 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(const int32_
       string_rows(offsets, j, n, &begin, &end);
       if (end - begin <= kShortString) continue;
       int32_t count = 0;
-#pragma unroll 4
-      for (int64_t t = begin + threadIdx.x; t < end; t += kThreads) count += is_scored(targets, t, vocab);
+      for (int64_t t0 = begin + threadIdx.x; t0 < end; t0 += kThreads * kEach) {
+        int32_t target[kEach];
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) target[k] = targets[min(t0 + k * kThreads, end - 1)];
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) count += t0 + k * kThreads < end && target[k] >= 0 && target[k] < vocab;
+      }
       count = sum_workgroup<kThreads>(count);
       const float w = weight_of(count);
 #pragma unroll 4
