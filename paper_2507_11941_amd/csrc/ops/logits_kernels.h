@@ -487,34 +487,36 @@ __device__ inline void rows_outside(const int64_t* offsets, int32_t batch, int64
 
 // One workgroup a pair: both sides' sums, in 64 bits as there are thousands of terms of either sign, the loss, and the factor of
 // each row's gradient.  One more: rows outside every string.  3 us for short strings, 6 for some hundreds of rows, again of waiting.
-__global__ void __launch_bounds__(256) pair_kernel(const float* logprobs, const int32_t* targets, int64_t n, int64_t vocab,
-                                                   const int64_t* offsets, int32_t batch, const float* reference, float beta,
-                                                   float smoothing, float scale, float* margins, double* losses, float* upstream) {
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads) pair_kernel(const float* logprobs, const int32_t* targets, int64_t n, int64_t vocab,
+                                                        const int64_t* offsets, int32_t batch, const float* reference, float beta,
+                                                        float smoothing, float scale, float* margins, double* losses,
+                                                        float* upstream) {
   const int32_t k = blockIdx.x;
-  if (k == batch / 2) return rows_outside<256>(offsets, batch, n, [&](int64_t t) { upstream[t] = 0.0f; });
+  if (k == batch / 2) return rows_outside<kThreads>(offsets, batch, n, [&](int64_t t) { upstream[t] = 0.0f; });
   int64_t begin, middle, end, unused;
   string_rows(offsets, 2 * k, n, &begin, &middle);
   string_rows(offsets, 2 * k + 1, n, &unused, &end);
   constexpr int kDeep = 4;
   double sum = 0.0;
-  for (int64_t t0 = begin + threadIdx.x; t0 < end; t0 += 256 * kDeep) {
+  for (int64_t t0 = begin + threadIdx.x; t0 < end; t0 += kThreads * kDeep) {
     int32_t target[kDeep];
     float lp[kDeep], ref[kDeep];
 #pragma unroll
     for (int k = 0; k < kDeep; ++k) {                        // (all reads side by side)
-      const int64_t t = min(t0 + k * 256, end - 1);
+      const int64_t t = min(t0 + k * kThreads, end - 1);
       target[k] = targets[t];
       lp[k] = logprobs[t];
       ref[k] = reference ? reference[t] : 0.0f;
     }
 #pragma unroll
     for (int k = 0; k < kDeep; ++k) {
-      const int64_t t = t0 + k * 256;
+      const int64_t t = t0 + k * kThreads;
       const double apart = (double)lp[k] - (double)ref[k];
       if (t < end && target[k] >= 0 && target[k] < vocab) sum += t < middle ? apart : -apart;
     }
   }
-  const double z = (double)beta * sum_workgroup<256>(sum);
+  const double z = (double)beta * sum_workgroup<kThreads>(sum);
   // -log sigmoid(z) = max(-z, 0) + log(1 + exp(-|z|))
   const double tail = log1p(exp(-fabs(z)));
   const double loss = (1.0 - (double)smoothing) * (fmax(-z, 0.0) + tail) + (double)smoothing * (fmax(z, 0.0) + tail);
@@ -524,34 +526,35 @@ __global__ void __launch_bounds__(256) pair_kernel(const float* logprobs, const 
     losses[k] = loss / (batch / 2);
     if (margins) margins[k] = (float)z;
   }
-  for (int64_t t = begin + threadIdx.x; t < end; t += 256) upstream[t] = t < middle ? c : -c;
+  for (int64_t t = begin + threadIdx.x; t < end; t += kThreads) upstream[t] = t < middle ? c : -c;
 }
 
 __global__ void __launch_bounds__(1024) sum_kernel(const double* values, int64_t n, float* sum) {
   sum_values<1024>(values, n, sum);
 }
 
-constexpr int kWeightWaves = 4;                              // strings of a workgroup
+constexpr int kWeightWaves = 4;                              // waves of a workgroup
 constexpr int kShortString = 1024;                           // positions that one wave goes over
 
 // The weight of each scored position in its string's loss and its advantage; and the number of scored positions of this
-// workgroup's strings.  A wave has a string, the whole workgroup one after the other those that are long.  The last workgroup:
-// rows outside every string.  4 us for short strings, 8 for some of hundreds of positions: reads that
-// wait for each other.
+// workgroup's strings.  `strings` of them, one a wave, or one where most are long; the whole workgroup goes over the long ones, one
+// after the other.  The last workgroup: rows outside every string.  4 us for short strings, 8 for some of hundreds of positions:
+// reads that wait for each other.
 __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(const int32_t* targets, int64_t n, int64_t vocab,
                                                                     const int64_t* offsets, int32_t batch, int by_string,
                                                                     const float* advantages, int advantage_by_string, float* weight,
-                                                                    float* advantage, int32_t* scored) {
-  constexpr int kThreads = 64 * kWeightWaves, kEach = kShortString / 64;
+                                                                    float* advantage, int32_t* scored, int strings) {
+  constexpr int kThreads = 64 * kWeightWaves, kEach = kShortString / 64, kHalf = kEach / 2;
   if (blockIdx.x == gridDim.x - 1) return rows_outside<kThreads>(offsets, batch, n, [&](int64_t t) { weight[t] = 0.0f; });
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const auto weight_of = [&](int32_t count) { return by_string ? 1.0f / ((float)batch * (float)max(count, 1)) : 1.0f; };
   int32_t all = 0;                                           // of the waves' strings, in lane 0 of each; of long ones in thread 0
-  for (int32_t i0 = blockIdx.x * kWeightWaves; i0 < batch; i0 += (gridDim.x - 1) * kWeightWaves) {
+  const int short_string = strings == 1 ? 64 : kShortString;
+  for (int32_t i0 = blockIdx.x * strings; i0 < batch; i0 += (gridDim.x - 1) * strings) {
     const int32_t i = i0 + wave;
     int64_t begin = 0, end = 0;
-    if (i < batch) string_rows(offsets, i, n, &begin, &end);
-    if (end - begin <= kShortString) {
+    if (wave < strings && i < batch) string_rows(offsets, i, n, &begin, &end);
+    if (end - begin <= short_string) {
       bool is[kEach];
       float adv[kEach];
       int32_t count = 0;
@@ -573,10 +576,10 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(const int32_
       }
       if (lane == 0) all += count;
     }
-    if (!__syncthreads_or(end - begin > kShortString)) continue;
-    for (int32_t j = i0; j < min(i0 + kWeightWaves, batch); ++j) {
+    if (!__syncthreads_or(end - begin > short_string)) continue;
+    for (int32_t j = i0; j < min(i0 + strings, batch); ++j) {
       string_rows(offsets, j, n, &begin, &end);
-      if (end - begin <= kShortString) continue;
+      if (end - begin <= short_string) continue;
       int32_t count = 0;
       for (int64_t t0 = begin + threadIdx.x; t0 < end; t0 += kThreads * kEach) {
         int32_t target[kEach];
@@ -587,10 +590,22 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(const int32_
       }
       count = sum_workgroup<kThreads>(count);
       const float w = weight_of(count);
-#pragma unroll 4
-      for (int64_t t = begin + threadIdx.x; t < end; t += kThreads) {
-        weight[t] = is_scored(targets, t, vocab) ? w : 0.0f;
-        advantage[t] = advantages[advantage_by_string ? j : t];
+      for (int64_t t0 = begin + threadIdx.x; t0 < end; t0 += kThreads * kHalf) {
+        int32_t target[kHalf];
+        float adv[kHalf];
+#pragma unroll
+        for (int k = 0; k < kHalf; ++k) {
+          const int64_t t = min(t0 + k * kThreads, end - 1);
+          target[k] = targets[t];
+          adv[k] = advantages[advantage_by_string ? j : t];
+        }
+#pragma unroll
+        for (int k = 0; k < kHalf; ++k) {
+          const int64_t t = t0 + k * kThreads;
+          if (t >= end) continue;
+          weight[t] = target[k] >= 0 && target[k] < vocab ? w : 0.0f;
+          advantage[t] = adv[k];
+        }
       }
       if (threadIdx.x == 0) all += count;
     }

@@ -99,7 +99,8 @@ def preference(lp, targets, offsets, vocab, reference, beta, smoothing):
     apart = torch.where(scored, lp - (torch.where(scored, reference.double(), 0.0) if reference is not None else 0.0), 0.0)
     sums = torch.stack([apart[string == i].sum() for i in range(len(offsets) - 1)]) if len(offsets) > 1 else torch.zeros(0)
     z = beta * (sums[0::2] - sums[1::2])
-    each = (1 - smoothing) * torch.log1p(torch.exp(-z)) + smoothing * torch.log1p(torch.exp(z))
+    zero = torch.zeros_like(z)                            # (exp(z) alone would overflow from 710 on)
+    each = (1 - smoothing) * torch.logaddexp(zero, -z) + smoothing * torch.logaddexp(zero, z)
     return (each.mean() if len(z) else each.sum()), z
 
 

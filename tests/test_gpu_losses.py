@@ -38,7 +38,7 @@ def test_next_tokens(lens, before, after):
 
 
 
-PAIRS = [[3, 4], [0, 5], [1, 1], [0, 0], [40, 7, 300, 512, 1, 0, 2, 2], [900, 1100]]
+PAIRS = [[3, 4], [0, 5], [1, 1], [0, 0], [40, 7, 300, 512, 1, 0, 2, 2], [900, 1100], [5000, 3, 0, 2600], [2049, 700]]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -108,7 +108,8 @@ def test_preference_of_far_apart_strings():
         assert torch.isfinite(grad).all() and bool(grad.any()) == (turn > 0)
 
 
-POLICIES = [[5], [3, 4, 0, 1], [0, 0], [64, 300, 1, 2, 700], [900], [1500, 3, 0, 1100, 1024]]
+POLICIES = [[5], [3, 4, 0, 1], [0, 0], [64, 300, 1, 2, 700], [900], [1500, 3, 0, 1100, 1024], [1500, 3, 0, 0, 1, 2, 1100, 1],
+            [9000, 2, 0, 4097, 63], [2049, 64, 65]]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
