@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(256) embed_kernel(const T* weight, int64_t voc
 // touches, in 32 bits in the workspace, and another kernel adds those.  Which rows are added in which order follows from the
 // sorted ids alone.
 //
-// Bound by memory: 65,536 rows of 2,048 bfloat16 into 100,260 rows of 32 bits, 1.08 GB, take 227 us (4.8 TB/s) after 26 us of
+// Bound by memory: 65,536 rows of 2,048 bfloat16 into 100,260 rows of 32 bits, 1.08 GB, take 219 to 232 us (4.7 to 4.9 TB/s) after 26 us of
 // sorting, and 10 us for the 184 tokens that have more than 32 rows.  Clearing the rows that no id names while the sort waits, before
 // the sums, or between them changed nothing beyond 1 %: reads that follow 0.7 GB of writes wait for these to leave the caches.
 

@@ -5,9 +5,9 @@
 // row stays in registers between the two), and once more in where the factor needs other rows.  Measured on one MI355X, whose
 // memory reads 6.2 to 6.3 TB/s, fills 6.9 to 7.3 and copies 5.0 (read and written):
 //   log-probabilities of 8,191 rows of 100,260 bfloat16 (1.64 GB)            264 us, 6.2 TB/s
-//   with the gradient, 8,209 rows of 32,256 bfloat16 (1.06 GB)               204 us, 5.2 TB/s
-//   policy loss, 8,190 rows of 100,260 bfloat16 (2.86 GB)                    570 us, 5.0 TB/s
-//   gradient from a saved lse, 8,003 rows of 100,260 bfloat16 (2.78 GB)      518 us, 5.4 TB/s
+//   with the gradient, 8,209 rows of 32,256 bfloat16 (1.06 GB)               203 us, 5.2 TB/s
+//   policy loss, 8,190 rows of 100,260 bfloat16 (2.86 GB)                    564 us, 5.1 TB/s
+//   gradient from a saved lse, 8,003 rows of 100,260 bfloat16 (2.78 GB)      522 us, 5.3 TB/s
 // An exponential costs as much as four other instructions: of 16-bit logits the first of these keeps the vector units busy nine
 // tenths of the time, and 32-bit ones, half as many a byte, come in at 6.3 TB/s.
 #pragma once
