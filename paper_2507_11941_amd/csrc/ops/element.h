@@ -24,19 +24,50 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 typedef uint32_t Words __attribute__((ext_vector_type(4)));
 
+// The same at any multiple of kBytes.
+template <int kBytes>
+struct At;
+template <>
+struct At<2> {
+  typedef uint32_t Type __attribute__((ext_vector_type(4), aligned(2)));
+};
+template <>
+struct At<4> {
+  typedef uint32_t Type __attribute__((ext_vector_type(4), aligned(4)));
+};
+
+template <bool kValue>
+struct Constant {
+  static constexpr bool value = kValue;
+};
+
+constexpr int kLine = 128;                                   // bytes of a cache line
+
+// How many of n elements lie before the first whole line of kBytes.
+template <int kBytes, typename T>
+__device__ inline int head_of(const T* p, int64_t n) {
+  return (int)min((int64_t)(-(uintptr_t)p % kBytes / sizeof(T)), n);
+}
+
 // 16 bytes of a row.
 template <typename T>
 struct Vec {
   static constexpr int kWidth = 16 / sizeof(T);
   Words w;
 
+  // With kOnce the access passes the caches by, as far as it can: for what nobody reads again soon.  Stores only where waves write
+  // whole lines: parts of one go to memory each by themselves.
+  template <bool kOnce = false>
   __device__ static Vec load(const T* p) {
-    struct __attribute__((packed, aligned(alignof(T)))) At { Words w; };
-    return {((const At*)p)->w};
+    typedef typename At<sizeof(T)>::Type Here;
+    if constexpr (kOnce) return {__builtin_nontemporal_load((const Here*)p)};
+    else return {*(const Here*)p};
   }
+  template <bool kOnce = false>
   __device__ void store(T* p) const {
-    struct __attribute__((packed, aligned(alignof(T)))) At { Words w; };
-    ((At*)p)->w = w;
+    typedef typename At<sizeof(T)>::Type Here;
+    if constexpr (kOnce) __builtin_nontemporal_store(w, (Here*)p);
+    else *(Here*)p = w;
   }
   __device__ void get(float (&x)[kWidth]) const {
     if constexpr (sizeof(T) == 4) {

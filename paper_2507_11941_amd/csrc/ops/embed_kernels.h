@@ -14,7 +14,7 @@ __device__ inline int64_t rows_in_use(int64_t n, const int64_t* count) {
 template <typename T, int kVecs>
 __global__ void __launch_bounds__(256) embed_kernel(const T* weight, int64_t vocab, int64_t dim, int64_t weight_stride,
                                                     const int32_t* ids, int64_t first, int64_t n, unsigned parts, const int64_t* count,
-                                                    float scale, T* out, int64_t out_stride) {
+                                                    float scale, T* out, int64_t out_stride, bool once) {
   constexpr int kWidth = Vec<T>::kWidth;
   const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   const int64_t t = first + wave / parts, begin = (int64_t)(wave % parts) * (kVecs * 64 * kWidth);
@@ -39,15 +39,19 @@ __global__ void __launch_bounds__(256) embed_kernel(const T* weight, int64_t voc
   for (int k = 0; k < kVecs; ++k)
     if (k * 64 + lane < whole) v[k] = Vec<T>::load(from + begin + (k * 64 + lane) * kWidth);
   if (has_last) to[last] = from_float<T>(scale * to_float(from[last]));
+  const auto write = [&](auto pass_by) {
 #pragma unroll
-  for (int k = 0; k < kVecs; ++k)
-    if (k * 64 + lane < whole) {
-      float x[kWidth];
-      v[k].get(x);
+    for (int k = 0; k < kVecs; ++k)
+      if (k * 64 + lane < whole) {
+        float x[kWidth];
+        v[k].get(x);
 #pragma unroll
-      for (int i = 0; i < kWidth; ++i) x[i] *= scale;
-      Vec<T>::of(x).store(to + begin + (k * 64 + lane) * kWidth);
-    }
+        for (int i = 0; i < kWidth; ++i) x[i] *= scale;
+        Vec<T>::of(x).template store<pass_by.value>(to + begin + (k * 64 + lane) * kWidth);
+      }
+  };
+  if (once) write(Constant<true>{});
+  else write(Constant<false>{});
 }
 
 // ---- the gradient --------------------------------------------------------------------------------------------
@@ -76,6 +80,7 @@ struct GradArgs {
   int64_t grad_stride, out_stride;
   float scale;
   int accumulate;
+  bool once;                                                 // grad's rows pass the caches by
   const uint8_t* present;                                    // whether there is a token; not used where it is accumulated
   uint32_t* long_runs;                                       // their number, cleared by the sort; then the chunks they begin in
   float* pieces;                                             // [chunks][2][dim]: of a run from before, of one that goes on
@@ -94,8 +99,9 @@ __device__ inline Columns columns_of(int64_t tile, int64_t dim) {
   return {max((int64_t)0, min(own, dim - kWidth)), own, min(own + kWidth, dim)};
 }
 
-template <typename T>
+template <typename T, bool kOnce>
 __device__ inline Vec<T> load_columns(const T* row, const Columns& c, int64_t dim) {
+  if constexpr (kOnce) return Vec<T>::template load<true>(row + c.load);
   if (dim >= Vec<T>::kWidth) return Vec<T>::load(row + c.load);
   float x[Vec<T>::kWidth] = {};
   for (int i = 0; i < Vec<T>::kWidth; ++i)
@@ -214,10 +220,15 @@ __global__ void __launch_bounds__(256) embed_grad_kernel(const T* grad, O* out, 
   float sum[kWidth] = {};
   for (int r0 = from; r0 < n_rows; r0 += kDeep) {
     Vec<T> v[kDeep];
+    const auto row = [&](int k) {
+      return grad + (int64_t)(uint32_t)__builtin_amdgcn_readlane(position, min(r0 + k, n_rows - 1)) * a.grad_stride;
+    };
+    if (a.once) {
 #pragma unroll
-    for (int k = 0; k < kDeep; ++k) {
-      const int r = min(r0 + k, n_rows - 1);
-      v[k] = load_columns(grad + (int64_t)(uint32_t)__builtin_amdgcn_readlane(position, r) * a.grad_stride, cols, a.dim);
+      for (int k = 0; k < kDeep; ++k) v[k] = load_columns<T, true>(row(k), cols, a.dim);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k) v[k] = load_columns<T, false>(row(k), cols, a.dim);
     }
 #pragma unroll
     for (int k = 0; k < kDeep; ++k) {

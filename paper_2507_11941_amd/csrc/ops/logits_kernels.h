@@ -89,7 +89,7 @@ __device__ inline Stats join_workgroup(Stats mine) {
 }
 
 // The statistics of this thread's part of the elements [begin, end) of a row, 16 bytes a lane, four loads in flight.
-template <typename T, int kThreads>
+template <typename T, int kThreads, bool kOnce>
 __device__ inline Stats stream(const T* x, int64_t begin, int64_t end) {
   constexpr int kWidth = Vec<T>::kWidth, kDeep = 4;
   Stats stats = {-INFINITY, 0.0f};
@@ -99,14 +99,14 @@ __device__ inline Stats stream(const T* x, int64_t begin, int64_t end) {
   for (; left >= kDeep * kThreads; left -= kDeep * kThreads, at += kDeep * kThreads * kWidth) {
     Vec<T> v[kDeep];
 #pragma unroll
-    for (int k = 0; k < kDeep; ++k) v[k] = Vec<T>::load(at + k * kThreads * kWidth);
+    for (int k = 0; k < kDeep; ++k) v[k] = Vec<T>::template load<kOnce>(at + k * kThreads * kWidth);
     absorb<T, kDeep>(stats, v);
   }
   Vec<T> v[kDeep];
 #pragma unroll
   for (int k = 0; k < kDeep; ++k) {
     v[k] = Vec<T>::all(-INFINITY);
-    if (k * kThreads + (int)threadIdx.x < left) v[k] = Vec<T>::load(at + k * kThreads * kWidth);
+    if (k * kThreads + (int)threadIdx.x < left) v[k] = Vec<T>::template load<kOnce>(at + k * kThreads * kWidth);
   }
   absorb<T, kDeep>(stats, v);
   if ((int)threadIdx.x < rest) stats = join(stats, {to_float(x[end - rest + (int)threadIdx.x]), 1.0f});
@@ -129,6 +129,7 @@ struct RowArgs {
   float* lse;                 // null: not wanted
   const float* upstream;      // kRowStep
   int64_t grad_stride;
+  bool once;                  // logits, and whole lines of the gradient, pass the caches by
   // kRowPolicy
   const float* weight;        // of each row's loss; 0: not scored
   const int32_t* scored;      // the numbers of scored rows whose sum the loss is divided by,
@@ -215,13 +216,18 @@ __device__ inline void skip_row(const RowArgs& a, int64_t t) {
   }
 }
 
+// Zeros: whole lines, and the elements before and behind them.
 template <typename T, int kThreads>
-__device__ inline void zero_row(T* g, int64_t vocab) {
+__device__ inline void zero_row(T* g, int64_t vocab, bool once) {
   constexpr int kWidth = Vec<T>::kWidth;
-  const int64_t whole = vocab / kWidth;
-  for (int64_t j = threadIdx.x; j < whole; j += kThreads) Vec<T>::all(0.0f).store(g + j * kWidth);
-  const int64_t j = whole * kWidth + threadIdx.x;
-  if (j < vocab) g[j] = from_float<T>(0.0f);
+  const int head = head_of<kLine>(g, vocab);
+  const int64_t whole = (vocab - head) / kWidth;
+  if (once)
+    for (int64_t j = threadIdx.x; j < whole; j += kThreads) Vec<T>::all(0.0f).template store<true>(g + head + j * kWidth);
+  else
+    for (int64_t j = threadIdx.x; j < whole; j += kThreads) Vec<T>::all(0.0f).store(g + head + j * kWidth);
+  const int edges = (int)(vocab - whole * kWidth);
+  for (int j = threadIdx.x; j < edges; j += kThreads) g[j < head ? j : whole * kWidth + j] = from_float<T>(0.0f);
 }
 
 // share x exp(x - reference) of the elements of a vector.
@@ -243,7 +249,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const T* logits, int
   if (!is_scored(in, vocab)) return skip_row<kRowLogprob>(a, t);
   const T* x = logits + t * stride;
   const float at_target = to_float(x[in.target]);
-  const Stats all = join_workgroup<kThreads>(stream<T, kThreads>(x, 0, vocab));
+  const Stats all = join_workgroup<kThreads>(a.once ? stream<T, kThreads, true>(x, 0, vocab) : stream<T, kThreads, false>(x, 0, vocab));
   if (threadIdx.x == 0) finish_row<kRowLogprob>(a, t, in, all, logprob_of(at_target, all));
 }
 
@@ -254,7 +260,7 @@ __global__ void __launch_bounds__(256) logprobs_part_kernel(const T* logits, int
   const int64_t t = blockIdx.x / parts, begin = blockIdx.x % parts * each, end = min(vocab, begin + each);
   const int32_t target = targets[t];
   if (target < 0 || target >= vocab) return;
-  const Stats all = join_workgroup<256>(stream<T, 256>(logits + t * stride, begin, end));
+  const Stats all = join_workgroup<256>(stream<T, 256, false>(logits + t * stride, begin, end));
   if (threadIdx.x == 0) part[blockIdx.x] = all;
 }
 
@@ -283,25 +289,35 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const T* logits, int64
   const RowInputs in = inputs_of<kKind>(a, t);
   if (!is_scored(in, vocab)) {
     skip_row<kKind>(a, t);
-    return zero_row<T, kThreads>(g, vocab);
+    return zero_row<T, kThreads>(g, vocab, a.once);
   }
   const T* x = logits + t * stride;
-  const int whole = (int)(vocab / kWidth), rest = (int)(vocab % kWidth);
-  const int lane_at = (int)threadIdx.x;
+  // Whole vectors from the row's first line on; the elements before and behind them, at most one a thread.  (Not from the
+  // gradient's first line on, which mostly is the same: sums would depend on where the gradient goes.)
+  constexpr int kBytes = kThreads == 64 ? 64 : kLine;
+  const int head = head_of<kBytes>(x, vocab), whole = ((int)vocab - head) / kWidth;
+  const int edges = (int)vocab - whole * kWidth, lane_at = (int)threadIdx.x;
+  const int edge_at = lane_at < head ? lane_at : whole * kWidth + lane_at;
   Vec<T> v[kVecs];
 #pragma unroll
-  for (int k = 0; k < kVecs; ++k) {
-    v[k] = Vec<T>::all(-INFINITY);
-    if (k * kThreads + lane_at < whole) v[k] = Vec<T>::load(x + (k * kThreads + lane_at) * kWidth);
+  for (int k = 0; k < kVecs; ++k) v[k] = Vec<T>::all(-INFINITY);
+  if (a.once) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k)
+      if (k * kThreads + lane_at < whole) v[k] = Vec<T>::template load<true>(x + head + (k * kThreads + lane_at) * kWidth);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k)
+      if (k * kThreads + lane_at < whole) v[k] = Vec<T>::load(x + head + (k * kThreads + lane_at) * kWidth);
   }
-  float last = -INFINITY;                                   // one of those behind the whole vectors
-  if (lane_at < rest) last = to_float(x[whole * kWidth + lane_at]);
+  float edge = -INFINITY;
+  if (lane_at < edges) edge = to_float(x[edge_at]);
   const float at_target = to_float(x[in.target]);
   Stats mine = {-INFINITY, 0.0f};
 #pragma unroll
   for (int k = 0; k + kDeep <= kVecs; k += kDeep) absorb<T, kDeep>(mine, v + k);
   if constexpr (kVecs % kDeep) absorb<T, kVecs % kDeep>(mine, v + kVecs / kDeep * kDeep);
-  const Stats all = join_workgroup<kThreads>(join(mine, {last, 1.0f}));
+  const Stats all = join_workgroup<kThreads>(join(mine, {edge, 1.0f}));
   if (threadIdx.x < 64) {
     const float lp = logprob_of(at_target, all);
     const float c = finish_row<kKind>(a, t, in, all, lp);
@@ -312,17 +328,24 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const T* logits, int64
   }
   __syncthreads();
   const float c = factor[0];
-  if (c == 0.0f) return zero_row<T, kThreads>(g, vocab);
+  if (c == 0.0f) return zero_row<T, kThreads>(g, vocab, a.once);
   const float share = -c / all.s;
   // (The logits are converted once more: kept as 32-bit numbers they would take twice the registers.)
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) asm("" : "+v"(v[k].w));
+  if (a.once && head == head_of<kBytes>(g, vocab)) {
 #pragma unroll
-  for (int k = 0; k < kVecs; ++k)
-    if (k * kThreads + lane_at < whole) grad_of(v[k], all.m, share).store(g + (k * kThreads + lane_at) * kWidth);
-  if (lane_at < rest) g[whole * kWidth + lane_at] = from_float<T>(share * exp_of(last, all.m));
+    for (int k = 0; k < kVecs; ++k)
+      if (k * kThreads + lane_at < whole) grad_of(v[k], all.m, share).template store<true>(g + head + (k * kThreads + lane_at) * kWidth);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k)
+      if (k * kThreads + lane_at < whole) grad_of(v[k], all.m, share).store(g + head + (k * kThreads + lane_at) * kWidth);
+  }
+  if (lane_at < edges) g[edge_at] = from_float<T>(share * exp_of(edge, all.m));
   // The target's element once more, by the thread that has just written it.
-  if (lane_at == (in.target < whole * kWidth ? in.target / kWidth % kThreads : in.target - whole * kWidth))
+  const int in_body = in.target - head;
+  if (in_body >= 0 && in_body < whole * kWidth ? lane_at == in_body / kWidth % kThreads : lane_at < edges && edge_at == in.target)
     g[in.target] = from_float<T>(factor[1]);
 }
 
@@ -336,11 +359,11 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const T* logits, int64_t
   const RowInputs in = inputs_of<kKind>(a, t);
   if (!is_scored(in, vocab)) {
     skip_row<kKind>(a, t);
-    return zero_row<T, kThreads>(g, vocab);
+    return zero_row<T, kThreads>(g, vocab, a.once);
   }
   const T* x = logits + t * stride;
   const float at_target = to_float(x[in.target]);
-  const Stats all = join_workgroup<kThreads>(stream<T, kThreads>(x, 0, vocab));
+  const Stats all = join_workgroup<kThreads>(stream<T, kThreads, false>(x, 0, vocab));
   if (threadIdx.x < 64) {
     const float lp = logprob_of(at_target, all);
     const float c = finish_row<kKind>(a, t, in, all, lp);
@@ -351,13 +374,20 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const T* logits, int64_t
   }
   __syncthreads();
   const float c = factor[0];
-  if (c == 0.0f) return zero_row<T, kThreads>(g, vocab);
+  if (c == 0.0f) return zero_row<T, kThreads>(g, vocab, a.once);
   const float share = -c / all.s;
-  const int64_t whole = vocab / kWidth;
-  for (int64_t j = threadIdx.x; j < whole; j += kThreads) grad_of(Vec<T>::load(x + j * kWidth), all.m, share).store(g + j * kWidth);
-  const int64_t j = whole * kWidth + threadIdx.x;
-  if (j < vocab) g[j] = from_float<T>(share * exp_of(to_float(x[j]), all.m));
-  if (threadIdx.x == (in.target < whole * kWidth ? in.target / kWidth % kThreads : in.target - whole * kWidth))
+  const int head = head_of<kLine>(g, vocab), lane_at = (int)threadIdx.x;
+  const int64_t whole = (vocab - head) / kWidth, edges = vocab - whole * kWidth;
+  if (a.once)
+    for (int64_t j = lane_at; j < whole; j += kThreads)
+      grad_of(Vec<T>::template load<true>(x + head + j * kWidth), all.m, share).template store<true>(g + head + j * kWidth);
+  else
+    for (int64_t j = lane_at; j < whole; j += kThreads)
+      grad_of(Vec<T>::load(x + head + j * kWidth), all.m, share).store(g + head + j * kWidth);
+  const int64_t edge_at = lane_at < head ? lane_at : whole * kWidth + lane_at;
+  if (lane_at < edges) g[edge_at] = from_float<T>(share * exp_of(to_float(x[edge_at]), all.m));
+  const int64_t in_body = in.target - head;
+  if (in_body >= 0 && in_body < whole * kWidth ? lane_at == in_body / kWidth % kThreads : lane_at < edges && edge_at == in.target)
     g[in.target] = from_float<T>(factor[1]);
 }
 
@@ -396,40 +426,55 @@ __device__ inline void sum_values(const double* values, int64_t n, float* sum) {
 template <typename T>
 __global__ void __launch_bounds__(256) logprobs_grad_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, unsigned parts,
                                                             const int32_t* targets, const float* lse, const float* upstream,
-                                                            T* grad, int64_t grad_stride, const double* losses, int32_t n_losses,
+                                                            T* grad, int64_t grad_stride, bool once, const double* losses, int32_t n_losses,
                                                             float* loss) {
   if (blockIdx.x == gridDim.x - 1 && loss) return sum_values<256>(losses, n_losses, loss);
   constexpr int kWidth = Vec<T>::kWidth, kDeep = 4;
-  const int64_t t = first + blockIdx.x / parts, begin = (int64_t)(blockIdx.x % parts) * (256 * kDeep * kWidth);
+  const int64_t t = first + blockIdx.x / parts;
+  const unsigned part = blockIdx.x % parts;
   const int32_t target = targets[t];
   const float c = target >= 0 && target < vocab ? upstream[t] : 0.0f;
-  const T* x = logits + t * stride + begin;
-  T* g = grad + t * grad_stride + begin;
-  const int64_t left = vocab - begin;
-  const int whole = (int)min(left / kWidth, (int64_t)(256 * kDeep)), at = threadIdx.x;
-  const int j = whole * kWidth + at;                        // one of those behind the whole vectors
-  const bool has_last = whole < 256 * kDeep && j < left;
+  const T* x = logits + t * stride;
+  T* g = grad + t * grad_stride;
+  // Whole vectors from the first line of the gradient's row on; the first part has the elements before them, the last those behind.
+  const int head = head_of<kLine>(g, vocab), at = threadIdx.x;
+  const int64_t begin = head + (int64_t)part * (256 * kDeep * kWidth), left = max(vocab - begin, (int64_t)0);
+  const int whole = (int)min(left / kWidth, (int64_t)(256 * kDeep));
+  int64_t edge_at = -1;
+  if (part == 0 && at < head) edge_at = at;
+  else if (whole < 256 * kDeep) {
+    const int64_t j = begin + whole * kWidth + at - (part == 0 ? head : 0);
+    if (j < vocab) edge_at = j;
+  }
   if (c == 0.0f) {
+    const auto clear = [&](auto pass_by) {
 #pragma unroll
-    for (int k = 0; k < kDeep; ++k)
-      if (k * 256 + at < whole) Vec<T>::all(0.0f).store(g + (k * 256 + at) * kWidth);
-    if (has_last) g[j] = from_float<T>(0.0f);
+      for (int k = 0; k < kDeep; ++k)
+        if (k * 256 + at < whole) Vec<T>::all(0.0f).template store<pass_by.value>(g + begin + (k * 256 + at) * kWidth);
+    };
+    if (once) clear(Constant<true>{});
+    else clear(Constant<false>{});
+    if (edge_at >= 0) g[edge_at] = from_float<T>(0.0f);
     return;
   }
   const float l = lse[t];
-  Vec<T> v[kDeep];
-#pragma unroll
-  for (int k = 0; k < kDeep; ++k)
-    if (k * 256 + at < whole) v[k] = Vec<T>::load(x + (k * 256 + at) * kWidth);
-  const int64_t target_at = target - begin;
-  const bool here = target_at >= 0 && (target_at < whole * kWidth ? target_at / kWidth % 256 == at : has_last && target_at == j);
+  const int64_t in_body = target - begin;
+  const bool here = in_body >= 0 && in_body < whole * kWidth ? in_body / kWidth % 256 == at : edge_at == target;
   float at_target = 0.0f;
-  if (here) at_target = to_float(x[target_at]);
-  if (has_last) g[j] = from_float<T>(-c * exp_of(to_float(x[j]), l));
+  const auto go = [&](auto pass_by) {
+    Vec<T> v[kDeep];
 #pragma unroll
-  for (int k = 0; k < kDeep; ++k)
-    if (k * 256 + at < whole) grad_of(v[k], l, -c).store(g + (k * 256 + at) * kWidth);
-  if (here) g[target_at] = from_float<T>(-c * expm1f(at_target - l));
+    for (int k = 0; k < kDeep; ++k)
+      if (k * 256 + at < whole) v[k] = Vec<T>::template load<pass_by.value>(x + begin + (k * 256 + at) * kWidth);
+    if (here) at_target = to_float(x[target]);
+    if (edge_at >= 0) g[edge_at] = from_float<T>(-c * exp_of(to_float(x[edge_at]), l));
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k)
+      if (k * 256 + at < whole) grad_of(v[k], l, -c).template store<pass_by.value>(g + begin + (k * 256 + at) * kWidth);
+  };
+  if (once) go(Constant<true>{});
+  else go(Constant<false>{});
+  if (here) g[target] = from_float<T>(-c * expm1f(at_target - l));
 }
 
 // ---- over strings --------------------------------------------------------------------------------------------

@@ -55,6 +55,20 @@ struct LogitsWorkspace {
   size_t parts, logprobs, values, upstream, advantage, counts, total;
 };
 
+// Whether what n rows of so many elements read and write passes the caches by: where it is more than the last level holds, 256 MB.
+// Passing by or not: a step of 8,209 rows of 32,256 bfloat16 181 and 204 us, 3,000 of 32,001 71 and 80, 1,600 (205 MB) 43 and 42, the
+// gradient alone of 800 (102 MB) 23 and 19, after their log-probabilities 38 and 32; of 3,000 of 32,001 float32 122 and 151.  A lookup
+// of 40,961 x 2,048 bfloat16 37 and 49, its gradient, of 65,536 rows, 241 and 266, of 10,000 x 1,024 float32 (41 MB) 50 and 48.
+bool passes_by(int64_t n, int64_t columns, size_t element_bytes) {
+  return (double)n * (double)columns * (double)element_bytes > 256e6;
+}
+
+// Whether rows begin with a line.
+template <typename T>
+bool rows_of_lines(const T* p, int64_t stride) {
+  return aligned(p, kLine) && stride * (int64_t)sizeof(T) % kLine == 0;
+}
+
 constexpr unsigned kWeightGroups = 256;                     // workgroups that count scored positions
 
 // Strings of 512 positions and more on average have more threads: 4 of 15,000 in 106 us a policy loss instead of 135 (of 1,256
@@ -102,11 +116,12 @@ constexpr int64_t kManyCopies = 32768;
 template <typename T>
 void launch_embed(const T* weight, int64_t vocab, int64_t dim, int64_t weight_stride, const int32_t* ids, int64_t n,
                   const int64_t* count, float scale, T* out, int64_t out_stride, hipStream_t stream) {
+  const bool once = passes_by(n, dim, 2 * sizeof(T)) && rows_of_lines(out, out_stride);
   const auto launch = [&](auto kernel, int vecs) {
     const int64_t columns = (int64_t)vecs * 64 * Vec<T>::kWidth, parts = (dim + columns - 1) / columns;
     for_rows(n, parts, [&](int64_t first, int64_t rows) {
       hipLaunchKernelGGL(kernel, dim3(blocks(rows * parts, 4)), dim3(256), 0, stream, weight, vocab, dim, weight_stride, ids, first, n,
-                         (unsigned)parts, count, scale, out, out_stride);
+                         (unsigned)parts, count, scale, out, out_stride, once);
     });
   };
   if (n * ((dim + 256 * Vec<T>::kWidth - 1) / (256 * Vec<T>::kWidth)) >= kManyCopies) launch(embed_kernel<T, 4>, 4);
@@ -177,6 +192,7 @@ template <typename T, typename O>
 void launch_embed_grad(const T* grad, O* out, GradArgs a, hipStream_t stream) {
   constexpr int64_t kMost = (int64_t)1 << 22;               // workgroups of a launch
   a.tiles = (unsigned)((a.dim + 64 * Vec<T>::kWidth - 1) / (64 * Vec<T>::kWidth));
+  a.once = passes_by(a.n, a.dim, sizeof(T)) && a.dim >= Vec<T>::kWidth && rows_of_lines(grad, a.grad_stride);
   const int64_t summing = (a.chunks * a.tiles + 3) / 4, row_vecs = (a.dim + Vec<O>::kWidth - 1) / Vec<O>::kWidth;
   const int64_t groups = summing + (a.accumulate ? 0 : ((int64_t)a.vocab * row_vecs + kClear - 1) / kClear);
   for (int64_t first = 0; first < groups; first += kMost)
@@ -189,7 +205,8 @@ void launch_embed_grad(const T* grad, O* out, GradArgs a, hipStream_t stream) {
 }
 
 template <typename T>
-void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, const RowArgs& a, Stats* part, hipStream_t stream) {
+void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, RowArgs a, Stats* part, hipStream_t stream) {
+  a.once = passes_by(n, vocab, sizeof(T));
   constexpr int64_t kStep = 256 * Vec<T>::kWidth;           // 4 KiB of a row
   const int64_t steps = (vocab + kStep - 1) / kStep;
   int64_t parts = splits_rows(n, steps) ? std::min(kParts / n, (steps + 1) / 2) : 1;
@@ -216,7 +233,8 @@ void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, 
 }
 
 template <typename T, int kKind>
-void launch_rows(const T* logits, int64_t n, int64_t vocab, int64_t stride, const RowArgs& a, T* grad, hipStream_t stream) {
+void launch_rows(const T* logits, int64_t n, int64_t vocab, int64_t stride, RowArgs a, T* grad, hipStream_t stream) {
+  a.once = passes_by(n, vocab, 2 * sizeof(T));
   // The smallest variant whose registers hold a row: threads x vectors a lane.  (25 vectors are what 128 registers have room for,
   // and with 128 two workgroups of 512 threads share a compute unit, the one loading while the other stores.)
   const int64_t vecs = vocab / Vec<T>::kWidth;
@@ -239,10 +257,11 @@ void launch_grad(const T* logits, int64_t n, int64_t vocab, int64_t stride, cons
                  const float* upstream, T* grad, int64_t grad_stride, hipStream_t stream, const double* losses = nullptr,
                  int32_t n_losses = 0, float* loss = nullptr) {
   const int64_t parts = (vocab / Vec<T>::kWidth + 1023) / 1024 + (vocab / Vec<T>::kWidth % 1024 == 0 && vocab % Vec<T>::kWidth);
+  const bool once = passes_by(n, vocab, 2 * sizeof(T));
   for_rows(n, parts, [&](int64_t first, int64_t rows) {
     float* const here = first == 0 ? loss : nullptr;
     hipLaunchKernelGGL(logprobs_grad_kernel<T>, dim3((unsigned)(rows * parts + (here ? 1 : 0))), dim3(256), 0, stream, logits, vocab,
-                       stride, first, (unsigned)parts, targets, lse, upstream, grad, grad_stride, losses, n_losses, here);
+                       stride, first, (unsigned)parts, targets, lse, upstream, grad, grad_stride, once, losses, n_losses, here);
   });
 }
 
