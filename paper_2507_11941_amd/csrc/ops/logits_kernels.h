@@ -423,10 +423,10 @@ __device__ inline void sum_values(const double* values, int64_t n, float* sum) {
 
 // The gradient from a saved lse: element by element, bound by memory.  A workgroup has up to 1,024 vectors of a row, one of its
 // `parts`.  With `loss`, one workgroup more: the loss is the sum of the pairs' losses.
-template <typename T>
+template <typename T, bool kOnce>
 __global__ void __launch_bounds__(256) logprobs_grad_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, unsigned parts,
                                                             const int32_t* targets, const float* lse, const float* upstream,
-                                                            T* grad, int64_t grad_stride, bool once, const double* losses, int32_t n_losses,
+                                                            T* grad, int64_t grad_stride, const double* losses, int32_t n_losses,
                                                             float* loss) {
   if (blockIdx.x == gridDim.x - 1 && loss) return sum_values<256>(losses, n_losses, loss);
   constexpr int kWidth = Vec<T>::kWidth, kDeep = 4;
@@ -447,33 +447,25 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(const T* logits, int
     if (j < vocab) edge_at = j;
   }
   if (c == 0.0f) {
-    const auto clear = [&](auto pass_by) {
 #pragma unroll
-      for (int k = 0; k < kDeep; ++k)
-        if (k * 256 + at < whole) Vec<T>::all(0.0f).template store<pass_by.value>(g + begin + (k * 256 + at) * kWidth);
-    };
-    if (once) clear(Constant<true>{});
-    else clear(Constant<false>{});
+    for (int k = 0; k < kDeep; ++k)
+      if (k * 256 + at < whole) Vec<T>::all(0.0f).template store<kOnce>(g + begin + (k * 256 + at) * kWidth);
     if (edge_at >= 0) g[edge_at] = from_float<T>(0.0f);
     return;
   }
   const float l = lse[t];
+  Vec<T> v[kDeep];
+#pragma unroll
+  for (int k = 0; k < kDeep; ++k)
+    if (k * 256 + at < whole) v[k] = Vec<T>::template load<kOnce>(x + begin + (k * 256 + at) * kWidth);
   const int64_t in_body = target - begin;
   const bool here = in_body >= 0 && in_body < whole * kWidth ? in_body / kWidth % 256 == at : edge_at == target;
   float at_target = 0.0f;
-  const auto go = [&](auto pass_by) {
-    Vec<T> v[kDeep];
+  if (here) at_target = to_float(x[target]);
+  if (edge_at >= 0) g[edge_at] = from_float<T>(-c * exp_of(to_float(x[edge_at]), l));
 #pragma unroll
-    for (int k = 0; k < kDeep; ++k)
-      if (k * 256 + at < whole) v[k] = Vec<T>::template load<pass_by.value>(x + begin + (k * 256 + at) * kWidth);
-    if (here) at_target = to_float(x[target]);
-    if (edge_at >= 0) g[edge_at] = from_float<T>(-c * exp_of(to_float(x[edge_at]), l));
-#pragma unroll
-    for (int k = 0; k < kDeep; ++k)
-      if (k * 256 + at < whole) grad_of(v[k], l, -c).template store<pass_by.value>(g + begin + (k * 256 + at) * kWidth);
-  };
-  if (once) go(Constant<true>{});
-  else go(Constant<false>{});
+  for (int k = 0; k < kDeep; ++k)
+    if (k * 256 + at < whole) grad_of(v[k], l, -c).template store<kOnce>(g + begin + (k * 256 + at) * kWidth);
   if (here) g[target] = from_float<T>(-c * expm1f(at_target - l));
 }
 

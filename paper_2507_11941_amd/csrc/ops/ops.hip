@@ -257,12 +257,15 @@ void launch_grad(const T* logits, int64_t n, int64_t vocab, int64_t stride, cons
                  const float* upstream, T* grad, int64_t grad_stride, hipStream_t stream, const double* losses = nullptr,
                  int32_t n_losses = 0, float* loss = nullptr) {
   const int64_t parts = (vocab / Vec<T>::kWidth + 1023) / 1024 + (vocab / Vec<T>::kWidth % 1024 == 0 && vocab % Vec<T>::kWidth);
-  const bool once = passes_by(n, vocab, 2 * sizeof(T));
-  for_rows(n, parts, [&](int64_t first, int64_t rows) {
-    float* const here = first == 0 ? loss : nullptr;
-    hipLaunchKernelGGL(logprobs_grad_kernel<T>, dim3((unsigned)(rows * parts + (here ? 1 : 0))), dim3(256), 0, stream, logits, vocab,
-                       stride, first, (unsigned)parts, targets, lse, upstream, grad, grad_stride, once, losses, n_losses, here);
-  });
+  const auto launch = [&](auto kernel) {
+    for_rows(n, parts, [&](int64_t first, int64_t rows) {
+      float* const here = first == 0 ? loss : nullptr;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * parts + (here ? 1 : 0))), dim3(256), 0, stream, logits, vocab, stride, first,
+                         (unsigned)parts, targets, lse, upstream, grad, grad_stride, losses, n_losses, here);
+    });
+  };
+  if (passes_by(n, vocab, 2 * sizeof(T))) launch(logprobs_grad_kernel<T, true>);
+  else launch(logprobs_grad_kernel<T, false>);
 }
 
 }  // namespace
