@@ -10,7 +10,8 @@ __device__ inline int64_t rows_in_use(int64_t n, const int64_t* count) {
 }
 
 // A lookup: a wave copies up to kVecs x 64 vectors of one row; a row takes `parts` waves.  Bound by memory: 40,961 rows of 2,048
-// bfloat16 of an embedding of 132 MB, which the last-level cache holds, in 42 us, 7.6 TB/s read and written.
+// bfloat16 of an embedding of 132 MB, which the last-level cache holds, in 36 us, 9.3 TB/s read and written
+// (42 us where what it writes takes that cache's place).
 template <typename T, int kVecs>
 __global__ void __launch_bounds__(256) embed_kernel(const T* weight, int64_t vocab, int64_t dim, int64_t weight_stride,
                                                     const int32_t* ids, int64_t first, int64_t n, unsigned parts, const int64_t* count,
@@ -62,8 +63,8 @@ __global__ void __launch_bounds__(256) embed_kernel(const T* weight, int64_t voc
 // touches, in 32 bits in the workspace, and another kernel adds those.  Which rows are added in which order follows from the
 // sorted ids alone.
 //
-// Bound by memory: 65,536 rows of 2,048 bfloat16 into 100,260 rows of 32 bits, 1.08 GB, take 219 to 232 us (4.7 to 4.9 TB/s) after 26 us of
-// sorting, and 10 us for the 184 tokens that have more than 32 rows.  Clearing the rows that no id names while the sort waits, before
+// Bound by memory: 65,536 rows of 2,048 bfloat16 into 100,260 rows of 32 bits, 1.08 GB, take 195 to 205 us (5.3 to 5.6 TB/s) after 26 us
+// of sorting, and 10 us for the 184 tokens that have more than 32 rows.  Clearing the rows that no id names while the sort waits, before
 // the sums, or between them changed nothing beyond 1 %: reads that follow 0.7 GB of writes wait for these to leave the caches.
 
 constexpr int kChunk = 32;                                   // positions of a chunk at most: a wave's lanes hold it and the next

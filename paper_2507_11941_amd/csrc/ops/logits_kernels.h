@@ -4,12 +4,14 @@
 // log-probabilities (a running maximum and sum), once in and once out for a gradient whose factor is known from the row itself (the
 // row stays in registers between the two), and once more in where the factor needs other rows.  Measured on one MI355X, whose
 // memory reads 6.2 to 6.3 TB/s, fills 6.9 to 7.3 and copies 5.0 (read and written):
-//   log-probabilities of 8,191 rows of 100,260 bfloat16 (1.64 GB)            264 us, 6.2 TB/s
-//   with the gradient, 8,209 rows of 32,256 bfloat16 (1.06 GB)               203 us, 5.2 TB/s
-//   policy loss, 8,190 rows of 100,260 bfloat16 (2.86 GB)                    564 us, 5.1 TB/s
-//   gradient from a saved lse, 8,003 rows of 100,260 bfloat16 (2.78 GB)      522 us, 5.3 TB/s
+//   log-probabilities of 8,191 rows of 100,260 bfloat16 (1.64 GB)            253 us, 6.5 TB/s
+//   with the gradient, 8,209 rows of 32,256 bfloat16 (1.06 GB)               176 us, 6.0 TB/s
+//   policy loss, 8,190 rows of 100,260 bfloat16 (2.86 GB)                    528 us, 5.4 TB/s
+//   gradient from a saved lse, 8,003 rows of 100,260 bfloat16 (2.78 GB)      519 us, 5.4 TB/s
 // An exponential costs as much as four other instructions: of 16-bit logits the first of these keeps the vector units busy nine
-// tenths of the time, and 32-bit ones, half as many a byte, come in at 6.3 TB/s.
+// tenths of the time, and 32-bit ones, half as many a byte, come in at 6.3 TB/s.  Where a call moves more than the last-level
+// cache holds, logits and gradients pass the caches by, which is how all but small calls come above the plain copy's rate; their
+// stores write whole lines then.
 #pragma once
 #include "element.h"
 
@@ -28,7 +30,7 @@ __device__ inline float exp_of(float x, float r) { return __builtin_amdgcn_exp2f
 
 // The same for term i of a sum.  log2 e lies between two 32-bit numbers, 1.34e-8 of itself above the one and 6.93e-8 below the
 // other.  With the nearer one alone all terms would be too large, and log-probabilities 1e-7 too low on average, which strings add
-// up; every sixth term takes the other, which makes up for it (a second product would cost 4 % of 8,191 x 100,260's 264 us).
+// up; every sixth term takes the other, which makes up for it (a second product would cost 4 % of 8,191 x 100,260's 253 us).
 __device__ inline float term_of(float x, float r, int i) {
   return __builtin_amdgcn_exp2f((x - r) * (i % 6 ? 1.44269502162933349609f : 1.44269514083862304688f));
 }
