@@ -220,3 +220,22 @@ def test_outputs_belong_to_the_stream_that_writes_them():
     grad = bpe.embed_tokens_grad(got, ids, 1000, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.equal(grad, grad_want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,stride", [(1024, 1024), (1000, 1024), (1000, 1000)])
+def test_more_than_the_caches_hold(dtype, dim, stride):
+    import paper_2507_11941_amd as bpe
+
+    vocab, n = 3000, 256_000_000 // (1000 * torch.empty(0, dtype=TYPES[dtype]).element_size()) + 1000
+    g = torch.Generator(device=dev()).manual_seed(1)
+    weight = torch.randn(vocab, dim, generator=g, device=dev()).to(TYPES[dtype])
+    ids = torch.randint(-1, vocab, (n,), generator=g, device=dev(), dtype=torch.int32)
+    out = torch.empty(n, stride, dtype=TYPES[dtype], device=dev())[:, :dim]
+    bpe.embed_tokens(weight, ids, out=out)
+    assert torch.equal(out, torch.where(ids[:, None] < 0, 0, weight[ids.long().clamp(min=0)]))
+    # Whole numbers of up to 8: sums are exact in any order.
+    out.copy_(torch.randint(-8, 9, (n, dim), generator=g, device=dev()))
+    got = bpe.embed_tokens_grad(out, ids, vocab, dtype=torch.float32)
+    want = torch.zeros(vocab + 1, dim, device=dev()).index_add_(0, torch.where(ids < 0, vocab, ids).long(), out.float())
+    assert torch.equal(got, want[:vocab])

@@ -206,6 +206,38 @@ def test_elements_beyond_32_bits():
     assert not x.any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,shift", [(33001, 0), (32256, 0), (32256, 1), (1000, 0)])
+def test_more_than_the_caches_hold(dtype, vocab, shift):
+    """A row's results do not depend on how many others there are, nor on whether they pass the caches by."""
+    import paper_2507_11941_amd as bpe
+
+    n = 256_000_000 // (vocab * torch.empty(0, dtype=TYPES[dtype]).element_size()) + 100
+    x, targets, upstream = some_logits(n, vocab, TYPES[dtype], 1), some_targets(n, vocab, 2), some_upstream(n, 3)
+    out = torch.empty(n * vocab + shift, dtype=TYPES[dtype], device=dev())[shift:].view(n, vocab)
+    lp, lse = bpe.token_logprobs(x, targets)
+    grad = bpe.token_logprobs_grad(x, targets, lse, upstream, out=out).clone()
+    lp1, lse1, grad1 = bpe.token_logprobs_and_grad(x, targets, upstream, out=out)
+    for rows in (slice(0, 70), slice(n // 2, n // 2 + 70), slice(n - 70, n)):
+        few = bpe.token_logprobs(x[rows], targets[rows])
+        assert torch.equal(few[0], lp[rows]) and torch.equal(few[1], lse[rows])
+        assert torch.equal(bpe.token_logprobs_grad(x[rows], targets[rows], few[1], upstream[rows]), grad[rows])
+        few = bpe.token_logprobs_and_grad(x[rows], targets[rows], upstream[rows])
+        assert torch.equal(few[0], lp1[rows]) and torch.equal(few[1], lse1[rows]) and torch.equal(few[2], grad1[rows])
+        check_all(x[rows], targets[rows], upstream[rows])
+    # In place, and a policy loss at the old policy, which is a step with -advantage / (number of scored tokens).
+    advantages = torch.where(upstream == 0, 1.0, upstream)
+    many = ((targets >= 0) & (targets < vocab)).sum()
+    offsets = torch.tensor([0, n], device=dev())
+    want = bpe.token_logprobs_and_grad(x, targets, -advantages / many)[2].float()
+    loss, lp2, got = bpe.policy_loss(x, targets, offsets, lp1, advantages, out=x)
+    assert torch.equal(lp2, lp1) and got.data_ptr() == x.data_ptr()
+    # (both divide, in another order, and round the gradient once)
+    ulp = {"f32": 2.0 ** -23, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[dtype]
+    off = want.abs() * (2 * ulp + 4 * 2.0 ** -23) + (2.0 ** -24 if dtype == "f16" else 0.0)
+    assert ((got.float() - want).abs() <= off).all()
+
+
 def test_another_stream_and_a_graph():
     import paper_2507_11941_amd as bpe
 
