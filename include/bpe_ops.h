@@ -112,6 +112,8 @@ int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab,
  *   advantages  float[n], or float[batch] with advantage_by_string != 0: one for all of a string.
  *   reference   float[n], or NULL: no KL term, and none where kl_weight is 0.
  *   old, reference and advantages are not read where a row is not scored; positions outside every string are not scored.
+ *               A NaN in those of a scored row, or for its log-probability, makes the loss NaN and the row's gradient; an
+ *               advantage of 0 has no part in the loss, whatever the ratio, unless that is NaN.
  *   scale, loss, logprobs, grad  as for bpe_preference_loss (but logprobs are 0 outside every string); loss = 0 where nothing
  *                                is scored. */
 int bpe_policy_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets,

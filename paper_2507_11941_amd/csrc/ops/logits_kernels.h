@@ -173,12 +173,15 @@ __device__ inline bool is_scored(const RowInputs& in, int64_t vocab) {
   return in.target >= 0 && in.target < vocab && in.weight != 0.0f;
 }
 
-// The loss of one token under the clipped policy, and its derivative with respect to the token's log-probability.
+// The loss of one token under the clipped policy, and its derivative with respect to the token's log-probability.  Comparisons that
+// keep a NaN: fminf and fmaxf would put the bound in the place of a ratio that is none.  An advantage of 0 has no part in the loss,
+// however large the ratio.
 __device__ inline float policy_value(const RowArgs& a, const RowInputs& in, float lp, float* slope) {
-  const float ratio = expf(lp - in.old);
-  const float free = ratio * in.advantage, clipped = fminf(fmaxf(ratio, 1.0f - a.low), 1.0f + a.high) * in.advantage;
-  float value = -fminf(free, clipped);
-  *slope = free <= clipped ? -free : 0.0f;
+  const float ratio = expf(lp - in.old), low = 1.0f - a.low, high = 1.0f + a.high;
+  const float clipped = (ratio < low ? low : ratio > high ? high : ratio) * in.advantage;
+  const float free = in.advantage == 0.0f ? clipped : ratio * in.advantage;
+  float value = clipped < free ? -clipped : -free;
+  *slope = clipped < free ? 0.0f : -free;
   if (a.reference) {
     const float d = in.reference - lp;
     value += a.kl_weight * (expm1f(d) - d);
