@@ -76,7 +76,7 @@ size_t bpe_token_logprobs_workspace_bytes(int64_t n, int64_t vocab);
  *   grad[t][j] = upstream[t] * ((j == targets[t]) - exp(logits[t][j] - lse[t])).
  * Rows that are not scored, and rows whose upstream is 0, get zeros and are not read.
  *   lse   as bpe_token_logprobs wrote it: 32 bits, which is 1e-6 of the gradient for logits of some tens and nothing left of
- *         it for logits of 10^7 (the one-pass form below keeps the maximum and the sum apart, and has no such limit).
+ *         it for logits of 10^7 (the one-pass form and the losses below keep the maximum and the sum apart, and have no such limit).
  *   grad  [n][vocab] of the logits' type; may be the logits themselves (same pointer and stride), else not overlapping. */
 int bpe_token_logprobs_grad(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets,
                             const float* lse, const float* upstream, void* grad, int64_t grad_stride, void* stream);

@@ -129,6 +129,7 @@ struct RowArgs {
   const int32_t* targets;
   float* logprobs;            // null: not wanted
   float* lse;                 // null: not wanted
+  Stats* stats;               // null: not wanted; of scored rows
   const float* upstream;      // kRowStep
   int64_t grad_stride;
   bool once;                  // logits, and whole lines of the gradient, pass the caches by
@@ -196,6 +197,7 @@ __device__ inline float finish_row(const RowArgs& a, int64_t t, const RowInputs&
   if (threadIdx.x == 0) {
     if (a.logprobs) a.logprobs[t] = lp;
     if (a.lse) a.lse[t] = lse_of(all);
+    if (a.stats) a.stats[t] = all;
   }
   if constexpr (kKind == kRowStep) return in.upstream;
   if constexpr (kKind == kRowPolicy) {
@@ -426,13 +428,15 @@ __device__ inline void sum_values(const double* values, int64_t n, float* sum) {
   if (threadIdx.x == 0) *sum = (float)mine;
 }
 
-// The gradient from a saved lse: element by element, bound by memory.  A workgroup has up to 1,024 vectors of a row, one of its
-// `parts`.  With `loss`, one workgroup more: the loss is the sum of the pairs' losses.
+// The gradient from what was saved of each row: element by element, bound by memory.  A workgroup has up to 1,024 vectors of a row,
+// one of its `parts`.  Saved is lse, the caller's, or, where it never leaves the library, `stats`: the maximum and the sum apart, as a
+// 32-bit lse of logits about 10^4 says their sum to 10^-3 only, and of the type's lowest value nothing.  With `loss`, one workgroup
+// more: the loss is the sum of the pairs' losses.
 template <typename T, bool kOnce>
 __global__ void __launch_bounds__(256) logprobs_grad_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, unsigned parts,
-                                                            const int32_t* targets, const float* lse, const float* upstream,
-                                                            T* grad, int64_t grad_stride, const double* losses, int32_t n_losses,
-                                                            float* loss) {
+                                                            const int32_t* targets, const float* lse, const Stats* stats,
+                                                            const float* upstream, T* grad, int64_t grad_stride, const double* losses,
+                                                            int32_t n_losses, float* loss) {
   if (blockIdx.x == gridDim.x - 1 && loss) return sum_values<256>(losses, n_losses, loss);
   constexpr int kWidth = Vec<T>::kWidth, kDeep = 4;
   const int64_t t = first + blockIdx.x / parts;
@@ -458,7 +462,8 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(const T* logits, int
     if (edge_at >= 0) g[edge_at] = from_float<T>(0.0f);
     return;
   }
-  const float l = lse[t];
+  const Stats all = stats ? stats[t] : Stats{lse[t], 1.0f};
+  const float share = -c / all.s;
   Vec<T> v[kDeep];
 #pragma unroll
   for (int k = 0; k < kDeep; ++k)
@@ -467,11 +472,11 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(const T* logits, int
   const bool here = in_body >= 0 && in_body < whole * kWidth ? in_body / kWidth % 256 == at : edge_at == target;
   float at_target = 0.0f;
   if (here) at_target = to_float(x[target]);
-  if (edge_at >= 0) g[edge_at] = from_float<T>(-c * exp_of(to_float(x[edge_at]), l));
+  if (edge_at >= 0) g[edge_at] = from_float<T>(share * exp_of(to_float(x[edge_at]), all.m));
 #pragma unroll
   for (int k = 0; k < kDeep; ++k)
-    if (k * 256 + at < whole) grad_of(v[k], l, -c).template store<kOnce>(g + begin + (k * 256 + at) * kWidth);
-  if (here) g[target] = from_float<T>(-c * expm1f(at_target - l));
+    if (k * 256 + at < whole) grad_of(v[k], all.m, share).template store<kOnce>(g + begin + (k * 256 + at) * kWidth);
+  if (here) g[target] = from_float<T>(-c * expm1f(logprob_of(at_target, all)));
 }
 
 // ---- over strings --------------------------------------------------------------------------------------------

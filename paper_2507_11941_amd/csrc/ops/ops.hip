@@ -50,7 +50,8 @@ size_t place(size_t& total, size_t bytes) {
   return at;
 }
 
-// The parts of the workspace of the functions on logits.
+// The parts of the workspace of the functions on logits.  `values` holds the rows' shares of the policy loss, 64 bits each, or the
+// rows' statistics for the preference loss's gradient; `advantage` the rows' advantages, or the pairs' losses, 64 bits each.
 struct LogitsWorkspace {
   size_t parts, logprobs, values, upstream, advantage, counts, total;
 };
@@ -95,9 +96,9 @@ LogitsWorkspace logits_layout(int64_t n, int64_t vocab, int32_t batch) {
   LogitsWorkspace w{};
   w.parts = place(w.total, parts_bytes(n, vocab));
   w.logprobs = place(w.total, (size_t)n * 4);
-  w.values = place(w.total, (size_t)std::max<int64_t>(n, batch) * 8);
+  w.values = place(w.total, (size_t)n * 8);
   w.upstream = place(w.total, (size_t)n * 4);
-  w.advantage = place(w.total, (size_t)n * 4);
+  w.advantage = place(w.total, (size_t)std::max<int64_t>(n, batch) * 4);
   w.counts = place(w.total, kWeightGroups * 4);
   return w;
 }
@@ -254,14 +255,14 @@ void launch_rows(const T* logits, int64_t n, int64_t vocab, int64_t stride, RowA
 
 template <typename T>
 void launch_grad(const T* logits, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets, const float* lse,
-                 const float* upstream, T* grad, int64_t grad_stride, hipStream_t stream, const double* losses = nullptr,
-                 int32_t n_losses = 0, float* loss = nullptr) {
+                 const Stats* stats, const float* upstream, T* grad, int64_t grad_stride, hipStream_t stream,
+                 const double* losses = nullptr, int32_t n_losses = 0, float* loss = nullptr) {
   const int64_t parts = (vocab / Vec<T>::kWidth + 1023) / 1024 + (vocab / Vec<T>::kWidth % 1024 == 0 && vocab % Vec<T>::kWidth);
   const auto launch = [&](auto kernel) {
     for_rows(n, parts, [&](int64_t first, int64_t rows) {
       float* const here = first == 0 ? loss : nullptr;
       hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * parts + (here ? 1 : 0))), dim3(256), 0, stream, logits, vocab, stride, first,
-                         (unsigned)parts, targets, lse, upstream, grad, grad_stride, losses, n_losses, here);
+                         (unsigned)parts, targets, lse, stats, upstream, grad, grad_stride, losses, n_losses, here);
     });
   };
   if (passes_by(n, vocab, 2 * sizeof(T))) launch(logprobs_grad_kernel<T, true>);
@@ -376,7 +377,7 @@ int bpe_token_logprobs_grad(const void* logits, int dtype, int64_t n, int64_t vo
   if (n == 0) return BPE_OK;
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    launch_grad((const T*)logits, n, vocab, stride, targets, lse, upstream, (T*)grad, grad_stride, (hipStream_t)stream);
+    launch_grad((const T*)logits, n, vocab, stride, targets, lse, nullptr, upstream, (T*)grad, grad_stride, (hipStream_t)stream);
   });
   return launched();
 }
@@ -415,13 +416,13 @@ int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab,
   const hipStream_t stream = (hipStream_t)stream_ptr;
   char* ws = (char*)workspace;
   float* lp = logprobs ? logprobs : (float*)(ws + w.logprobs);
-  double* losses = (double*)(ws + w.values);
+  double* losses = (double*)(ws + w.advantage);
   float* upstream = (float*)(ws + w.upstream);
-  float* lse = (float*)(ws + w.advantage);
+  Stats* stats = (Stats*)(ws + w.values);
   RowArgs a{};
   a.targets = targets;
   a.logprobs = lp;
-  a.lse = lse;
+  a.stats = stats;
   with_type(dtype, [&](auto type) {
     using T = decltype(type);
     if (n > 0) launch_logprobs((const T*)logits, n, vocab, stride, a, (Stats*)(ws + w.parts), stream);
@@ -432,7 +433,8 @@ int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab,
     if (long_strings(n, batch)) launch_pairs(pair_kernel<1024>, 1024);
     else if (batch > 0 || n > 0) launch_pairs(pair_kernel<256>, 256);
     if (n > 0)
-      launch_grad((const T*)logits, n, vocab, stride, targets, lse, upstream, (T*)grad, grad_stride, stream, losses, batch / 2, loss);
+      launch_grad((const T*)logits, n, vocab, stride, targets, nullptr, stats, upstream, (T*)grad, grad_stride, stream, losses, batch / 2,
+                  loss);
     else
       hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(1024), 0, stream, losses, (int64_t)(batch / 2), loss);
   });
