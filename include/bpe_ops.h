@@ -99,7 +99,8 @@ size_t bpe_loss_workspace_bytes(int64_t n, int64_t vocab, int32_t batch);
  *   scale      factor of the gradient (loss scaling, weight of the loss); the loss itself is not scaled.
  *   loss       one float; 0 for no pairs.  margins float[batch/2], logprobs float[n]: either may be NULL.
  *   grad       as above; rows outside every string get zeros (and have logprobs all the same).  A string without scored
- *              positions has S = 0. */
+ *              positions has S = 0.  A masked target makes S -inf: its pair adds 0 or infinity to the loss (a term whose
+ *              weight is 0 is left out), and where it adds 0 its gradient is 0. */
 int bpe_preference_loss(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* targets,
                         const int64_t* offsets, int32_t batch, const float* reference, float beta, float smoothing,
                         float scale, float* loss, float* margins, float* logprobs, void* grad, int64_t grad_stride,

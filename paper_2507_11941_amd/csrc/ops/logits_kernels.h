@@ -564,10 +564,11 @@ __global__ void __launch_bounds__(kThreads) pair_kernel(const float* logprobs, c
     }
   }
   const double z = (double)beta * sum_workgroup<kThreads>(sum);
-  // -log sigmoid(z) = max(-z, 0) + log(1 + exp(-|z|))
-  const double tail = log1p(exp(-fabs(z)));
-  const double loss = (1.0 - (double)smoothing) * (fmax(-z, 0.0) + tail) + (double)smoothing * (fmax(z, 0.0) + tail);
-  const double slope = (double)smoothing - 1.0 / (1.0 + exp(z));
+  // -log sigmoid(z) = max(-z, 0) + log(1 + exp(-|z|)).  A masked target makes z infinite and one of the two terms with it: left out
+  // where its weight is 0.  (tail is NaN where z is.)
+  const double tail = log1p(exp(-fabs(z))), less = (double)smoothing;
+  const double loss = tail + (less < 1.0 ? (1.0 - less) * fmax(-z, 0.0) : 0.0) + (less > 0.0 ? less * fmax(z, 0.0) : 0.0);
+  const double slope = less - 1.0 / (1.0 + exp(z));
   const float c = (float)((double)scale * (double)beta * slope / (batch / 2));
   if (threadIdx.x == 0) {
     losses[k] = loss / (batch / 2);
