@@ -48,8 +48,8 @@ __device__ inline Stats join(Stats a, Stats b) {
   return {m, a.s * change_of(a.m, r) + b.s * change_of(b.m, r)};
 }
 
-// Some more of a row's logits: one maximum and one change of reference for all of them.  Sums are in 32 bits: a lane adds up to 100
-// terms to one of two sums, and some ten steps join the lanes.
+// Some more of a row's logits: one maximum and one change of reference for all of them.  Sums are in 32 bits: half of the terms are
+// added to the sum so far, one after another.  That are 128 of them at most, and some ten steps join the lanes.
 template <typename T, int kVecs>
 __device__ inline void absorb(Stats& stats, const Vec<T>* v) {
   constexpr int kWidth = Vec<T>::kWidth;
@@ -90,8 +90,9 @@ __device__ inline Stats join_workgroup(Stats mine) {
   return mine;
 }
 
-// The statistics of this thread's part of the elements [begin, end) of a row, 16 bytes a lane, four loads in flight.
-template <typename T, int kThreads, bool kOnce>
+// The statistics of this thread's part of the elements [begin, end) of a row, 16 bytes a lane, four loads in flight.  With kEven
+// nothing is done for the part of a step behind whole ones where there is none.
+template <typename T, int kThreads, bool kOnce, bool kEven = false>
 __device__ inline Stats stream(const T* x, int64_t begin, int64_t end) {
   constexpr int kWidth = Vec<T>::kWidth, kDeep = 4;
   Stats stats = {-INFINITY, 0.0f};
@@ -104,6 +105,7 @@ __device__ inline Stats stream(const T* x, int64_t begin, int64_t end) {
     for (int k = 0; k < kDeep; ++k) v[k] = Vec<T>::template load<kOnce>(at + k * kThreads * kWidth);
     absorb<T, kDeep>(stats, v);
   }
+  if (kEven && left == 0 && rest == 0) return stats;
   Vec<T> v[kDeep];
 #pragma unroll
   for (int k = 0; k < kDeep; ++k) {
@@ -113,6 +115,23 @@ __device__ inline Stats stream(const T* x, int64_t begin, int64_t end) {
   absorb<T, kDeep>(stats, v);
   if ((int)threadIdx.x < rest) stats = join(stats, {to_float(x[end - rest + (int)threadIdx.x]), 1.0f});
   return stats;
+}
+
+// The same for any length.  Terms that are alike err alike, and of tens of millions of them added one after another 32 bits lose a
+// thousandth: the sums of kStretch elements a thread, which are 128 additions, are added in 64 bits.
+constexpr int kStretch = 256;
+
+template <typename T, int kThreads, bool kOnce>
+__device__ inline Stats stream_long(const T* x, int64_t begin, int64_t end) {
+  double sum = 0.0;
+  float m = -INFINITY;
+  for (; begin < end; begin += kThreads * kStretch) {
+    const Stats some = stream<T, kThreads, kOnce, true>(x, begin, min(end, begin + kThreads * kStretch));
+    const float to = fmaxf(m, some.m), r = reference_of(to);
+    sum = sum * (double)change_of(m, r) + (double)(some.s * change_of(some.m, r));
+    m = to;
+  }
+  return {m, (float)sum};
 }
 
 // The logarithm of a token's probability.  The difference first, which is exact or nearly so: of logits that are all the type's
@@ -249,25 +268,29 @@ __device__ inline Vec<T> grad_of(const Vec<T>& v, float reference, float share) 
 
 // Log-probabilities alone, one workgroup a row: bound by memory (see above); a single row by its compute unit's exponentials, 9 us
 // for 100,260.
-template <typename T, int kThreads>
+template <typename T, int kThreads, bool kLong>
 __global__ void __launch_bounds__(kThreads) logprobs_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, RowArgs a) {
   const int64_t t = first + blockIdx.x;
   const RowInputs in = inputs_of<kRowLogprob>(a, t);
   if (!is_scored(in, vocab)) return skip_row<kRowLogprob>(a, t);
   const T* x = logits + t * stride;
   const float at_target = to_float(x[in.target]);
-  const Stats all = join_workgroup<kThreads>(a.once ? stream<T, kThreads, true>(x, 0, vocab) : stream<T, kThreads, false>(x, 0, vocab));
+  Stats mine;
+  if constexpr (kLong) mine = a.once ? stream_long<T, kThreads, true>(x, 0, vocab) : stream_long<T, kThreads, false>(x, 0, vocab);
+  else mine = a.once ? stream<T, kThreads, true>(x, 0, vocab) : stream<T, kThreads, false>(x, 0, vocab);
+  const Stats all = join_workgroup<kThreads>(mine);
   if (threadIdx.x == 0) finish_row<kRowLogprob>(a, t, in, all, logprob_of(at_target, all));
 }
 
 // Few rows: each is split among `parts` workgroups, whose statistics another kernel joins.
-template <typename T>
+template <typename T, bool kLong>
 __global__ void __launch_bounds__(256) logprobs_part_kernel(const T* logits, int64_t vocab, int64_t stride, const int32_t* targets,
                                                             unsigned parts, int64_t each, Stats* part) {
   const int64_t t = blockIdx.x / parts, begin = blockIdx.x % parts * each, end = min(vocab, begin + each);
   const int32_t target = targets[t];
   if (target < 0 || target >= vocab) return;
-  const Stats all = join_workgroup<256>(stream<T, 256, false>(logits + t * stride, begin, end));
+  const T* x = logits + t * stride;
+  const Stats all = join_workgroup<256>(kLong ? stream_long<T, 256, false>(x, begin, end) : stream<T, 256, false>(x, begin, end));
   if (threadIdx.x == 0) part[blockIdx.x] = all;
 }
 
@@ -370,7 +393,7 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const T* logits, int64_t
   }
   const T* x = logits + t * stride;
   const float at_target = to_float(x[in.target]);
-  const Stats all = join_workgroup<kThreads>(stream<T, kThreads, false>(x, 0, vocab));
+  const Stats all = join_workgroup<kThreads>(stream_long<T, kThreads, false>(x, 0, vocab));
   if (threadIdx.x < 64) {
     const float lp = logprob_of(at_target, all);
     const float c = finish_row<kKind>(a, t, in, all, lp);

@@ -221,15 +221,20 @@ void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, 
       // The more threads a row has, the less of the chip is idle when the last rows end, and the more of a short row's time
       // goes into joining them.  8,191 rows of 200 KB with 256, 512, 1,024 threads: 277, 273, 263 us; of 129 KB 176, 173, 167; of
       // 64 KB 92.7, 89.5, 91.4; of 2.5 KB 19.6, 33.9, 67.7, with 64 threads 10.8.
-      if (steps >= 24) launch(logprobs_kernel<T, 1024>, 1024);
-      else if (steps >= 4) launch(logprobs_kernel<T, 512>, 512);
-      else if (steps >= 2) launch(logprobs_kernel<T, 256>, 256);
-      else launch(logprobs_kernel<T, 64>, 64);
+      if (vocab > 1024 * kStretch) launch(logprobs_kernel<T, 1024, true>, 1024);
+      else if (steps >= 24) launch(logprobs_kernel<T, 1024, false>, 1024);
+      else if (steps >= 4) launch(logprobs_kernel<T, 512, false>, 512);
+      else if (steps >= 2) launch(logprobs_kernel<T, 256, false>, 256);
+      else launch(logprobs_kernel<T, 64, false>, 64);
     });
     return;
   }
-  hipLaunchKernelGGL(logprobs_part_kernel<T>, dim3((unsigned)(n * parts)), dim3(256), 0, stream, logits, vocab, stride, a.targets,
-                     (unsigned)parts, each, part);
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(n * parts)), dim3(256), 0, stream, logits, vocab, stride, a.targets, (unsigned)parts, each,
+                       part);
+  };
+  if (each > 256 * kStretch) launch(logprobs_part_kernel<T, true>);
+  else launch(logprobs_part_kernel<T, false>);
   hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)n), dim3(64), 0, stream, logits, vocab, stride, (int)parts, part, a);
 }
 
