@@ -200,9 +200,11 @@ void launch_embed_grad(const T* grad, O* out, GradArgs a, hipStream_t stream) {
     hipLaunchKernelGGL((embed_grad_kernel<T, O>), dim3((unsigned)std::min(kMost, groups - first)), dim3(256), 0, stream, grad, out, a, first,
                        summing);
   const int64_t long_runs = a.n / (a.chunk + 1);            // at most
-  if (long_runs > 0)
-    hipLaunchKernelGGL((embed_grad_join_kernel<T, O>), dim3((unsigned)std::min<int64_t>(2048, long_runs * a.tiles)), dim3(256), 0, stream, out,
-                       a);
+  const auto join = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(2048, long_runs * a.tiles)), dim3(256), 0, stream, out, a);
+  };
+  if (a.chunks > kLongPieces) join(embed_grad_join_kernel<T, O, true>);
+  else if (long_runs > 0) join(embed_grad_join_kernel<T, O, false>);
 }
 
 template <typename T>
