@@ -2,7 +2,10 @@
 
 Every function enqueues on ``stream`` (default: torch's current stream of the tensors' device) and synchronises nothing.
 Outputs and workspaces that are not given are allocated, on that stream.  Matrices may have any stride between rows, but not
-between columns; vectors are contiguous.  What the kernels cannot take is refused (ValueError), never copied into shape."""
+between columns; vectors are contiguous.  What the kernels cannot take is refused (ValueError), never copied into shape.
+
+``embed_tokens`` is recorded by torch's automatic differentiation where its weight wants a gradient.  The functions on logits are not:
+their gradient is an output, which ``logits.backward(grad)`` hands on, and log-probabilities and losses carry none."""
 from __future__ import annotations
 
 import ctypes
@@ -10,11 +13,11 @@ import ctypes
 from ._binding import _check, load_library
 
 _TYPES = {}                                      # torch dtype -> the library's number of it
-_lib = torch = None                              # (the package can be imported without torch)
+_lib = torch = _Lookup = None                    # (the package can be imported without torch)
 
 
 def _load():
-    global _lib, torch
+    global _lib, torch, _Lookup
     if _lib is None:
         import torch as module
 
@@ -39,9 +42,28 @@ def _load():
         lib.bpe_token_logprobs_workspace_bytes.restype = sz
         lib.bpe_loss_workspace_bytes.argtypes = [i64, i64, i32]
         lib.bpe_loss_workspace_bytes.restype = sz
+        _Lookup = _lookup()
         _TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
         _lib = lib
     return _lib
+
+
+def _lookup():
+    """embed_tokens as torch's automatic differentiation knows it."""
+    class Lookup(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, weight, ids, scale, count):
+            ctx.save_for_backward(ids, count)
+            ctx.vocab, ctx.scale = weight.shape[0], scale
+            return embed_tokens(weight, ids, scale, count)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad):
+            ids, count = ctx.saved_tensors
+            return embed_tokens_grad(grad.contiguous(), ids, ctx.vocab, ctx.scale, count), None, None, None
+
+    return Lookup
 
 
 def _matrix(t, what, dev=None, shape=None, dtype=None):
@@ -128,10 +150,15 @@ def _count(count, dev):
 def embed_tokens(weight, ids, scale: float = 1.0, count=None, out=None, stream=None):
     """``out[t] = scale * weight[ids[t]]``: rows of an embedding [vocab, dim] for int32 ids [n]; zeros for an id outside the
     vocabulary (padding).  ``count``: one int64 on the GPU, from which row on ids and out are left alone (``out_offsets[-1:]``
-    of an encoded batch, whose ids need not all be in use)."""
+    of an encoded batch, whose ids need not all be in use).  A weight that wants a gradient gets it from the backward pass, in its
+    own type; ``out`` cannot be given then."""
     if stream is not None:
         return _on(stream, embed_tokens, weight, ids, scale, count, out)
     lib = _lib or _load()
+    if weight.requires_grad and torch.is_grad_enabled():
+        if out is not None:
+            raise ValueError("out cannot be recorded by automatic differentiation: give weight.detach(), or call under torch.no_grad()")
+        return _Lookup.apply(weight, ids, scale, count)
     stride, dev = _matrix(weight, "weight"), weight.device
     n, dim = ids.numel(), weight.shape[1]
     ids_ptr = _vector(ids, "ids", dev, torch.int32, None)
