@@ -150,6 +150,14 @@ def build_table_vocab(byte_ids, merges, merged_ids) -> Table:
     return Table(handle.value, len(m))
 
 
+def _written(*tensors):
+    """Tells torch that a kernel writes into tensors of the caller's: what has saved one for a gradient refuses to use it then.
+    (torch.autograd.graph.increment_version without its own checks: 0.2 us instead of 0.4.)"""
+    import torch
+
+    torch._C._increment_version(tensors)
+
+
 def workspace_bytes(batch: int, total_bytes: int, max_len: int) -> int:
     return int(load_library().bpe_workspace_bytes(batch, total_bytes, max_len))
 
@@ -171,6 +179,7 @@ def encode_batch(table: Table, data, offsets, max_len: int, out_ids=None, out_of
     batch = offsets.numel() - 1
     total = data.numel()
     dev = data.device
+    given = [t for t in (out_ids, out_offsets) if t is not None]
     if out_ids is None:
         out_ids = torch.empty(max(total, 1), dtype=torch.int32, device=dev)
     if out_offsets is None:
@@ -191,6 +200,8 @@ def encode_batch(table: Table, data, offsets, max_len: int, out_ids=None, out_of
                                 out_ids.data_ptr(), out_offsets.data_ptr(), workspace.data_ptr(),
                                 workspace.numel(), stream.cuda_stream)
     _check(code, "bpe_encode_batch")
+    if given:
+        _written(*given)
     return out_ids, out_offsets
 
 
@@ -219,6 +230,7 @@ def encode_batch_static(table: Table, data, offsets, max_len: int, out_ids, out_
     code = lib.bpe_encode_batch_static(table.handle, data.data_ptr(), offsets.data_ptr(), batch, data.numel(),
                                        max_len, out_ids.data_ptr(), out_offsets.data_ptr(), stream.cuda_stream)
     _check(code, "bpe_encode_batch_static")
+    _written(out_ids, out_offsets)
     return out_ids, out_offsets
 
 

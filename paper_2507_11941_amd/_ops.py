@@ -13,11 +13,11 @@ import ctypes
 from ._binding import _check, load_library
 
 _TYPES = {}                                      # torch dtype -> the library's number of it
-_lib = torch = _Lookup = None                    # (the package can be imported without torch)
+_lib = torch = _Lookup = _written = None         # (the package can be imported without torch)
 
 
 def _load():
-    global _lib, torch, _Lookup
+    global _lib, torch, _Lookup, _written
     if _lib is None:
         import torch as module
 
@@ -43,6 +43,7 @@ def _load():
         lib.bpe_loss_workspace_bytes.argtypes = [i64, i64, i32]
         lib.bpe_loss_workspace_bytes.restype = sz
         _Lookup = _lookup()
+        _written = torch._C._increment_version   # (as in _binding.py; a call's own tensors only, given as a tuple)
         _TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
         _lib = lib
     return _lib
@@ -166,6 +167,7 @@ def embed_tokens(weight, ids, scale: float = 1.0, count=None, out=None, stream=N
         out, out_stride = weight.new_empty((n, dim)), dim
     else:
         out_stride = _matrix(out, "out", dev, (n, dim), weight.dtype)
+        _written((out,))
     _enqueue(lib.bpe_embed_tokens, dev, weight.data_ptr(), _TYPES[weight.dtype], weight.shape[0], dim, stride, ids_ptr, n,
              None if count is None else _count(count, dev), scale, out.data_ptr(), out_stride)
     return out
@@ -182,6 +184,7 @@ def embed_tokens_grad(grad, ids, vocab: int, scale: float = 1.0, count=None, out
     stride, dev = _matrix(grad, "grad"), grad.device
     n, dim = grad.shape
     ids_ptr = _vector(ids, "ids", dev, torch.int32, n)
+    given = out
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -193,6 +196,8 @@ def embed_tokens_grad(grad, ids, vocab: int, scale: float = 1.0, count=None, out
     out_stride = _matrix(out, "out", dev, (vocab, dim))
     count_ptr = _count(count, dev)
     workspace = _workspace(workspace, lib.bpe_embed_tokens_grad_workspace_bytes(n, vocab, dim), dev, "embed_tokens_grad")
+    if given is not None:
+        _written((out,))
     _enqueue(lib.bpe_embed_tokens_grad, dev, grad.data_ptr(), _TYPES[grad.dtype], stride, ids_ptr, n, count_ptr, vocab, dim, scale,
              1 if accumulate else 0, out.data_ptr(), _TYPES[out.dtype], out_stride, workspace.data_ptr(), workspace.numel())
     return out
@@ -212,7 +217,11 @@ def next_tokens(ids, offsets, first=None, out=None, stream=None):
     first_ptr = None if first is None else _vector(first, "first", dev, torch.int32, batch)
     if out is None:
         out = torch.empty_like(ids)
-    _enqueue(lib.bpe_next_tokens, dev, ids_ptr, n, offsets_ptr, batch, first_ptr, _vector(out, "out", dev, torch.int32, n))
+        out_ptr = out.data_ptr()
+    else:
+        out_ptr = _vector(out, "out", dev, torch.int32, n)
+        _written((out,))
+    _enqueue(lib.bpe_next_tokens, dev, ids_ptr, n, offsets_ptr, batch, first_ptr, out_ptr)
     return out
 
 
@@ -221,7 +230,9 @@ def _grad_of(logits, out):
     if out is None:
         out = torch.empty_like(logits, memory_format=torch.contiguous_format)
         return out, out.shape[1]
-    return out, _matrix(out, "out", logits.device, tuple(logits.shape), logits.dtype)
+    stride = _matrix(out, "out", logits.device, tuple(logits.shape), logits.dtype)
+    _written((out,))
+    return out, stride
 
 
 def token_logprobs(logits, targets, workspace=None, stream=None):
