@@ -3,7 +3,7 @@ NaN, as the formula's are, and no other row is touched by it.  What is large or 
 import pytest
 import torch
 
-from ops_reference import TYPES, U, assert_near
+from ops_reference import LOG_SUM, TYPES, U, assert_near
 from test_gpu_logits import dev, some_logits
 
 pytestmark = pytest.mark.gpu
@@ -73,3 +73,22 @@ def test_large_ratios_and_masked_targets(dtype):
         share = torch.tensor([[1.0, 0.0]]) if masked else torch.tensor([[0.5, -0.5]])
         want = torch.zeros(1, 2) if slope == 0 else slope * share
         assert_near(grad, want, 0.0, f"gradient of {masked, advantage, old}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [7, 1256, 100260, 204809])
+def test_rows_of_the_lowest_value(dtype, vocab):
+    """Logits that are all the type's lowest value are all as likely: log-probability -log vocab, ratio 1."""
+    import paper_2507_11941_amd as bpe
+
+    x = torch.full((3, vocab), torch.finfo(TYPES[dtype]).min, dtype=TYPES[dtype], device=dev())
+    targets, offsets = torch.tensor([0, vocab // 2, vocab - 1], dtype=torch.int32, device=dev()), torch.tensor([0, 1, 3], device=dev())
+    even = torch.full((3,), 1 / vocab, dtype=torch.float64)
+    advantages = torch.tensor([1.0, -2.0, 0.5])
+    loss, lp, grad = bpe.policy_loss(x, targets, offsets, even.log().float().to(dev()), advantages.to(dev()), scale=3.0)
+    near = LOG_SUM + 2 * U * torch.tensor(vocab).log().item()         # of a log-probability and an old one
+    assert_near(lp, even.log(), LOG_SUM, "logprobs")
+    assert_near(loss, torch.tensor(0.5 / 3, dtype=torch.float64), 3.5 / 3 * (near + 8 * U), "loss")
+    want = (advantages.double() * 3 / 3)[:, None] * even[:, None].expand(3, vocab)
+    want[torch.arange(3), targets.cpu().long()] -= advantages.double()
+    assert_near(grad, want, want.abs() * (2 * near + 16 * U), "gradient")
