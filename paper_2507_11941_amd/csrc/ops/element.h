@@ -1,10 +1,10 @@
 // Types of the matrices that the operators on token batches read and write: float, bfloat16, half.  Everything is computed in
 // 32 bits; a result is rounded once, to nearest even, where it is stored.
 //
-// Rows are read and written 16 bytes a lane from the row's first element on, whatever its address: rows of a vocabulary of
-// 100,260 tokens begin at every multiple of 8 bytes, and a view may begin at any element.  The hardware takes such addresses
-// in global memory; a row that is read from its own 16-byte boundaries instead needs a head, a tail and, where the gradient's
-// rows lie differently, a second way to write.
+// Rows are read and written 16 bytes a lane, whatever their address: rows of a vocabulary of 100,260 tokens begin at every multiple
+// of 8 bytes, and a view may begin at any element.  The hardware takes such addresses in global memory.  What is only read, and rows
+// of an embedding, are taken from their first element on; what writes a gradient takes a row's vectors from its first whole line on,
+// with a head and a tail of single elements, as stores that pass the caches by have to write whole lines.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -4,10 +4,10 @@
 // log-probabilities (a running maximum and sum), once in and once out for a gradient whose factor is known from the row itself (the
 // row stays in registers between the two), and once more in where the factor needs other rows.  Measured on one MI355X, whose
 // memory reads 6.2 to 6.3 TB/s, fills 6.9 to 7.3 and copies 5.0 (read and written):
-//   log-probabilities of 8,191 rows of 100,260 bfloat16 (1.64 GB)            253 us, 6.5 TB/s
+//   log-probabilities of 8,191 rows of 100,260 bfloat16 (1.64 GB)            253 to 263 us from box to box, 6.2 to 6.5 TB/s
 //   with the gradient, 8,209 rows of 32,256 bfloat16 (1.06 GB)               176 us, 6.0 TB/s
-//   policy loss, 8,190 rows of 100,260 bfloat16 (2.86 GB)                    528 us, 5.4 TB/s
-//   gradient from a saved lse, 8,003 rows of 100,260 bfloat16 (2.78 GB)      519 us, 5.4 TB/s
+//   policy loss, 8,190 rows of 100,260 bfloat16 (2.86 GB)                    528 to 533 us, 5.4 TB/s
+//   gradient from what was saved, 8,003 rows of 100,260 bfloat16 (2.78 GB)   507 to 519 us, 5.4 to 5.5 TB/s
 // An exponential costs as much as four other instructions: of 16-bit logits the first of these keeps the vector units busy nine
 // tenths of the time, and 32-bit ones, half as many a byte, come in at 6.3 TB/s.  Where a call moves more than the last-level
 // cache holds, logits and gradients pass the caches by, which is how all but small calls come above the plain copy's rate; their
@@ -309,7 +309,10 @@ __global__ void __launch_bounds__(64) logprobs_join_kernel(const T* logits, int6
 }
 
 // Log-probability and gradient of a row in one pass: the row stays in the workgroup's registers, kVecs x 16 bytes a lane, at most
-// 128 registers in all.  One barrier for the statistics and one for the row's factor, which the first wave works out.
+// 128 registers in all.  One barrier for the statistics and one for the row's factor, which the first wave works out.  Workgroups of
+// 512 threads share a compute unit by two, the one loading while the other stores; one of 1,024 has it to itself, and its loads,
+// exponentials and stores follow each other (3,000 rows of 100,260 float32 in 430 us, 5.6 TB/s, of 128,256 bfloat16 in 309, 5.0).
+// The last of a lane's vectors does not pass the caches by: the compiler makes one plain access of both branches' last.
 template <typename T, int kKind, int kThreads, int kVecs>
 __global__ void __launch_bounds__(kThreads, 4) row_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, RowArgs a, T* grad) {
   constexpr int kWidth = Vec<T>::kWidth, kDeep = kVecs < 4 || (kVecs > 16 && sizeof(T) == 2) ? 2 : 4;
@@ -379,7 +382,8 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const T* logits, int64
     g[in.target] = from_float<T>(factor[1]);
 }
 
-// The same for rows that no workgroup's registers hold (over 400 KiB): they are read twice.
+// The same for rows that no workgroup's registers hold (over 400 KiB): they are read twice, first plainly, so that the second reading
+// may find some of it in the caches (3,000 rows of 300,007 bfloat16: 826 us, 6.5 TB/s with both).
 template <typename T, int kKind>
 __global__ void __launch_bounds__(1024) long_row_kernel(const T* logits, int64_t vocab, int64_t stride, int64_t first, RowArgs a, T* grad) {
   constexpr int kWidth = Vec<T>::kWidth, kThreads = 1024;

@@ -78,10 +78,15 @@ constexpr unsigned kWeightGroups = 256;                     // workgroups that c
 bool long_strings(int64_t n, int32_t batch) { return batch > 0 && n / batch >= 512; }
 
 // Few long rows are split among workgroups, as many as to make about kParts of them in all, and a second launch joins them.
-// Each has 4 KiB of a row in one step.  Of 8 rows of 126, 196, 392 and 3,906 KiB the log-probabilities take 5.8, 6.2, 6.5 and
-// 13.2 us in a graph, each by one workgroup 4.4, 9.8, 9.3 and 85; called one by one, where a launch costs the host 3.4 us,
-// 12.4, 12.1, 11.9 and 12.8 against 9.7, 9.8, 9.3 and 85.  100 rows: called one by one 12.7, 11.9, 13.3, 75 against 9.6, 11.4,
-// 16.3 and 110; 250 rows 12.2, 16.7 and 24.4 against 9.4, 14.9 and 21.3.
+// Each has 4 KiB of a row in one step.  Split and by one workgroup a row, us called one by one, where a launch costs the host 3.4, and
+// in a graph:
+//                 8 rows                   32 rows                  100 rows                 250 rows
+//     63 KiB      12.4,  9.7;  5.8,  4.4   12.6,  9.6;  6.3,  4.8   12.7,  9.6;  8.2,  5.7   12.2,  9.4; 10.8,  6.9
+//    196 KiB      12.1,  9.8;  6.2,  9.8   12.2, 10.4;  8.2, 10.4   11.9, 11.4; 11.6, 11.9   16.7, 14.9; 17.2, 15.3
+//    392 KiB      11.9,  9.3;  6.5,  9.3   12.2, 12.9;  9.8, 13.0   13.3, 16.3; 13.6, 16.4   24.4, 21.3; 24.9, 21.7
+//  3,906 KiB      12.8, 85.5; 13.2, 85.4   27.9, 88.4; 28.7, 89.4   75.2,  110; 78.1,  120
+// So from 256 KiB on, where it gains called one by one and in a graph, but for the fewest rows, which lose a second launch as they are
+// called; rows of 196 KiB gain in a graph alone, and are not split.
 constexpr int64_t kParts = 1024;
 constexpr int64_t kSplitBelow = 200, kSplitFrom = 64;       // rows; steps
 
@@ -220,9 +225,10 @@ void launch_logprobs(const T* logits, int64_t n, int64_t vocab, int64_t stride, 
       const auto launch = [&](auto kernel, int threads) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, stream, logits, vocab, stride, first, a);
       };
-      // The more threads a row has, the less of the chip is idle when the last rows end, and the more of a short row's time
+      // The more threads a row has, the less of the chip is idle when the last of many rows end, and the more of a short row's time
       // goes into joining them.  8,191 rows of 200 KB with 256, 512, 1,024 threads: 277, 273, 263 us; of 129 KB 176, 173, 167; of
-      // 64 KB 92.7, 89.5, 91.4; of 2.5 KB 19.6, 33.9, 67.7, with 64 threads 10.8.
+      // 64 KB 92.7, 89.5, 91.4; of 2.5 KB 19.6, 33.9, 67.7, with 64 threads 10.8.  Chosen by the length alone, which is not best for
+      // all numbers of rows: 600 of 200 KB take 27.1, 29.9, 32.4, 1,021 41.1, 39.8, 43.5, 2,100 79.2, 78.3, 78.9, 3,000 107, 106, 105.
       if (vocab > 1024 * kStretch) launch(logprobs_kernel<T, 1024, true>, 1024);
       else if (steps >= 24) launch(logprobs_kernel<T, 1024, false>, 1024);
       else if (steps >= 4) launch(logprobs_kernel<T, 512, false>, 512);
@@ -244,7 +250,7 @@ template <typename T, int kKind>
 void launch_rows(const T* logits, int64_t n, int64_t vocab, int64_t stride, RowArgs a, T* grad, hipStream_t stream) {
   a.once = passes_by(n, vocab, 2 * sizeof(T));
   // The smallest variant whose registers hold a row: threads x vectors a lane.  (25 vectors are what 128 registers have room for,
-  // and with 128 two workgroups of 512 threads share a compute unit, the one loading while the other stores.)
+  // and with 128 two workgroups of 512 threads share a compute unit, the one loading while the other stores; one of 1,024 is alone.)
   const int64_t vecs = vocab / Vec<T>::kWidth;
   for_rows(n, 1, [&](int64_t first, int64_t rows) {
     const auto launch = [&](auto kernel, int threads) {
