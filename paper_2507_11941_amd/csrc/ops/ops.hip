@@ -6,49 +6,13 @@
 #include <cstddef>
 
 #include "../../../include/bpe_ops.h"
+#include "arguments.h"
 #include "embed_kernels.h"
 #include "logits_kernels.h"
 
 using namespace bpe;
 
 namespace {
-
-int launched() { return hipGetLastError() == hipSuccess ? BPE_OK : BPE_EHIP; }
-
-size_t size_of(int dtype) { return dtype == BPE_F32 ? 4 : 2; }
-
-bool is_type(int dtype) { return dtype == BPE_F32 || dtype == BPE_BF16 || dtype == BPE_F16; }
-
-// Whether p may be used for n values of `size` bytes.
-bool fits(const void* p, int64_t n, size_t size) { return (n == 0 || p) && ((uintptr_t)p & (size - 1)) == 0; }
-
-// ... and, if there is one, an optional array.
-bool aligned(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) == 0; }
-
-bool is_matrix(const void* p, int dtype, int64_t rows, int64_t columns, int64_t stride) {
-  return is_type(dtype) && columns >= 1 && columns <= BPE_MAX_COLUMNS && stride >= columns && stride < ((int64_t)1 << 40) &&
-         fits(p, rows, size_of(dtype));
-}
-
-bool is_count(int64_t n) { return n >= 0 && n <= BPE_MAX_TOKENS; }
-
-bool is_workspace(const void* p, size_t bytes, size_t need) { return p && ((uintptr_t)p & 255) == 0 && bytes >= need && need > 0; }
-
-unsigned blocks(int64_t n, int64_t each) { return (unsigned)((n + each - 1) / each); }
-
-// Calls f with a value of the type.
-template <typename F>
-void with_type(int dtype, F&& f) {
-  if (dtype == BPE_F32) f(float{});
-  else if (dtype == BPE_BF16) f(bf16{});
-  else f(f16{});
-}
-
-size_t place(size_t& total, size_t bytes) {
-  const size_t at = total;
-  total += (bytes + 255) & ~(size_t)255;
-  return at;
-}
 
 // The parts of the workspace of the functions on logits.  `values` holds the rows' shares of the policy loss, 64 bits each, or the
 // rows' statistics for the preference loss's gradient; `advantage` the rows' advantages, or the pairs' losses, 64 bits each.
