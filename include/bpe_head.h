@@ -57,8 +57,11 @@ int bpe_quantize_rows(const void* x, int dtype, int64_t n, int64_t dim, int64_t 
 /* out[t][v] = scales[t] * weight_scales[v] * (sum over k of q[t][k] weight[v][k]); the sum is exact.
  *   q       int8 [n][dim], dim <= BPE_MAX_DIM_8BIT (the sum fits 32 bits);  scales float[n]
  *   weight  int8 [vocab][dim];  weight_scales float[vocab]
- *   out     [n][vocab] of `dtype`, overlapping nothing. */
+ *           both with a stride of at most BPE_MAX_STRIDE_8BIT
+ *   out     [n][vocab] of `dtype`, overlapping nothing.
+ * Rows that begin at multiples of 4 bytes and have a multiple of 4 columns are read fastest, at multiples of 128 bytes more so. */
 #define BPE_MAX_DIM_8BIT 131071
+#define BPE_MAX_STRIDE_8BIT 0xfffffe
 int bpe_project_8bit(const int8_t* q, int64_t n, int64_t dim, int64_t q_stride, const float* scales, const int8_t* weight,
                      int64_t vocab, int64_t weight_stride, const float* weight_scales, void* out, int dtype, int64_t out_stride,
                      void* stream);

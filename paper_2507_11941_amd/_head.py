@@ -119,9 +119,11 @@ def _bytes(t, what, dev=None, columns=None):
         raise ValueError(f"{what} must be an int8 matrix{'' if columns is None else f' of {columns} columns'}")
     row, column = t.stride()
     if t.shape[0] <= 1:
-        row = max(row, t.shape[1])
+        row = t.shape[1]
     if (column != 1 and t.shape[1] > 1) or row < t.shape[1]:
         raise ValueError(f"{what}: the columns of a row must lie side by side, and rows must not overlap")
+    if row > 0xfffffe:
+        raise ValueError(f"{what}: there are {row} bytes from row to row, more than 0xfffffe")
     return row
 
 

@@ -12,30 +12,78 @@ using namespace bpe;
 
 namespace {
 
-template <typename T, int kMt, int kVt, int kWm, int kWv, int kStages>
+// Tiles of tokens x vocabulary: by eight waves, one workgroup on a compute unit (256 x 256); by eight, two (128 x 128); by four, two
+// (64 x 64).
+enum Size { kLarge, kMiddle, kSmall };
+
+constexpr struct {
+  int tokens, words, at_once;
+} kSizes[] = {{256, 256, 256}, {128, 128, 512}, {64, 64, 512}};
+
+int64_t tiles_of(Size size, int64_t n, int64_t vocab) {
+  return (n + kSizes[size].tokens - 1) / kSizes[size].tokens * ((vocab + kSizes[size].words - 1) / kSizes[size].words);
+}
+
+// How long tiles of a size take, in rounds of middle ones.
+double rounds_of(Size size, int64_t n, int64_t vocab) {
+  constexpr double kRound[] = {1.7, 1.0, 0.8};
+  return kRound[size] * (double)((tiles_of(size, n, vocab) + kSizes[size].at_once - 1) / kSizes[size].at_once);
+}
+
+Size size_of_tiles(int64_t n, int64_t vocab) {
+  if (n <= 64) return kSmall;
+  Size best = kLarge;
+  for (Size size : {kMiddle, kSmall})
+    if (rounds_of(size, n, vocab) < rounds_of(best, n, vocab)) best = size;
+  return best;
+}
+
+// As many workgroups as the chip holds at once go through the tiles.
+template <typename T, Size kSize, int kMt, int kVt, int kWm, int kWv, int kStages>
 void launch_tiles(ProjectArgs a, bool direct, T* out, hipStream_t stream) {
-  constexpr int kTokens = 32 * kMt * kWm, kWords = 32 * kVt * kWv;
-  a.token_tiles = blocks(a.n, kTokens);
-  a.tiles = a.token_tiles * blocks(a.vocab, kWords);
+  static_assert(kSizes[kSize].tokens == 32 * kMt * kWm && kSizes[kSize].words == 32 * kVt * kWv);
+  a.token_tiles = blocks(a.n, kSizes[kSize].tokens);
+  a.tiles = (unsigned)tiles_of(kSize, a.n, a.vocab);
   const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(a.tiles), dim3(64 * kWm * kWv), 0, stream, a, out);
+    hipLaunchKernelGGL(kernel, dim3(std::min(a.tiles, (unsigned)kSizes[kSize].at_once)), dim3(64 * kWm * kWv), 0, stream, a, out);
   };
-  if (direct) launch(project_kernel<T, kMt, kVt, kWm, kWv, kStages, true>);
-  else launch(project_kernel<T, kMt, kVt, kWm, kWv, 2, false>);
+  if (direct) launch(project_kernel<T, kMt, kVt, kWm, kWv, kStages, 128, true>);
+  else launch(project_kernel<T, kMt, kVt, kWm, kWv, 2, 128, false>);
 }
 
 template <typename T>
-void launch_project(const ProjectArgs& a, T* out, hipStream_t stream) {
-  const auto in_sixteens = [](const void* p, int64_t stride) { return (((uintptr_t)p | (uintptr_t)stride) & 15) == 0; };
-  const bool direct = in_sixteens(a.q, a.q_stride) && in_sixteens(a.weight, a.weight_stride);
-  if (a.n <= 32) launch_tiles<T, 1, 1, 1, 4, 4>(a, direct, out, stream);
-  else if (a.n <= 64) launch_tiles<T, 2, 1, 1, 4, 3>(a, direct, out, stream);
-  else if (a.n <= 128) launch_tiles<T, 2, 2, 2, 2, 2>(a, direct, out, stream);
-  else launch_tiles<T, 4, 2, 2, 4, 2>(a, direct, out, stream);
+void launch_size(Size size, const ProjectArgs& a, bool direct, T* out, hipStream_t stream) {
+  if (size == kLarge) launch_tiles<T, kLarge, 4, 2, 2, 4, 2>(a, direct, out, stream);
+  else if (size == kMiddle) launch_tiles<T, kMiddle, 2, 1, 2, 4, 2>(a, direct, out, stream);
+  else launch_tiles<T, kSmall, 1, 1, 2, 2, 4>(a, direct, out, stream);
 }
 
+template <typename T>
+void launch_project(ProjectArgs a, T* out, hipStream_t stream) {
+  const auto in_fours = [](const void* p, int64_t stride) { return (((uintptr_t)p | (uintptr_t)stride) & 3) == 0; };
+  const bool direct = a.dim % 4 == 0 && a.dim >= 16 && in_fours(a.q, a.q_stride) && in_fours(a.weight, a.weight_stride);
+  const Size size = size_of_tiles(a.n, a.vocab);
+  // A last round that few workgroups have tiles of goes to smaller ones, in a second launch, where that takes less.
+  const int64_t token_tiles = (a.n + kSizes[size].tokens - 1) / kSizes[size].tokens, tiles = tiles_of(size, a.n, a.vocab);
+  const int64_t whole = tiles / kSizes[size].at_once * kSizes[size].at_once / token_tiles * kSizes[size].words;
+  if (size < kSmall && whole > 0 && whole < a.vocab) {
+    const Size rest = size_of_tiles(a.n, a.vocab - whole);
+    constexpr double kLaunch = 0.2;
+    if (rest > size && rounds_of(size, a.n, whole) + rounds_of(rest, a.n, a.vocab - whole) + kLaunch < rounds_of(size, a.n, a.vocab)) {
+      ProjectArgs last = a;
+      last.vocab -= whole;
+      last.weight += whole * a.weight_stride;
+      last.weight_scales += whole;
+      a.vocab = whole;
+      launch_size(rest, last, direct, out + whole, stream);
+    }
+  }
+  launch_size(size, a, direct, out, stream);
+}
+
+// (The rows of a tile are found by 32-bit offsets.)
 bool is_bytes(const void* p, int64_t rows, int64_t columns, int64_t stride) {
-  return stride >= columns && stride < ((int64_t)1 << 40) && fits(p, rows, 1);
+  return stride >= columns && stride <= BPE_MAX_STRIDE_8BIT && fits(p, rows, 1);
 }
 
 }  // namespace

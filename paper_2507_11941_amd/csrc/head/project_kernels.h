@@ -2,7 +2,7 @@
 //
 // A workgroup has a tile of tokens x vocabulary and goes along the columns in steps of 128 bytes a row, which wait in shared memory in
 // stages: while the matrix units work on one, the next are on their way.  The vocabulary is the matrix instruction's first operand,
-// so that a lane holds four neighbours of a token's logits, and the tile goes to memory through shared memory, 16 bytes a lane.
+// so that a lane holds four neighbours of a token's logits, and these go to memory through shared memory, 16 bytes a lane.
 #pragma once
 #include "../ops/element.h"
 
@@ -11,10 +11,7 @@ namespace bpe {
 typedef int Bytes16 __attribute__((ext_vector_type(4)));
 typedef int Sums __attribute__((ext_vector_type(16)));
 
-constexpr int kStep = 128;                                  // bytes of a row in a stage
 constexpr int kXcds = 8;
-
-__device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};
 
 struct ProjectArgs {
   const int8_t* q;
@@ -32,7 +29,7 @@ struct Tile {
   unsigned token, word;
 };
 
-constexpr unsigned kBand = 8;
+constexpr unsigned kBand = 4;
 
 __device__ inline Tile tile_of(unsigned block, unsigned token_tiles, unsigned tiles) {
   const unsigned die = block % kXcds, share = tiles / kXcds, more = tiles % kXcds;
@@ -42,10 +39,29 @@ __device__ inline Tile tile_of(unsigned block, unsigned token_tiles, unsigned ti
   return {band * kBand + in % height, in / height};
 }
 
+// Waits until at most kLeft of this wave's transfers are on their way (they end in the order of their beginning), then for all waves.
 template <int kLeft>
 __device__ inline void wait_and_meet() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLeft) : "memory");
+  static_assert(kLeft < 64);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((kLeft & 15) | 7 << 4 | (kLeft >> 4) << 14);     // ... and for its accesses to shared memory
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
+
+// From memory into shared memory, 16 or 4 bytes a lane, one lane behind the other from `to` on.
+template <int kBytes>
+__device__ inline void transfer(const void* from, void* to) {
+  static_assert(kBytes == 16 || kBytes == 4);
+  const auto* source = (const __attribute__((address_space(1))) void*)from;
+  auto* target = (__attribute__((address_space(3))) void*)to;
+  if constexpr (kBytes == 16) __builtin_amdgcn_global_load_lds(source, target, 16, 0, 0);
+  else __builtin_amdgcn_global_load_lds(source, target, 4, 0, 0);
+}
+
+// How far the chunks of 16 bytes of a row are turned.
+template <int kStep>
+__device__ inline int turn(int row) { return kStep == 128 ? row >> 1 & 7 : row >> 2 & 3; }
 
 // 16 bytes at any address.
 __device__ inline Bytes16 load_bytes(const int8_t* p) {
@@ -53,75 +69,116 @@ __device__ inline Bytes16 load_bytes(const int8_t* p) {
   return *(const Here*)p;
 }
 
-// The first `valid` of them, and zeros.
-__device__ inline Bytes16 load_some_bytes(const int8_t* p, int valid) {
-  if (valid >= 16) return load_bytes(p);
+// The 16 bytes from `at` on of a row of `dim`; zeros from its end on, behind which nothing is read: the row's last 16 bytes, shifted.
+__device__ inline Bytes16 load_end(const int8_t* row, int at, int dim) {
   Bytes16 v = {0, 0, 0, 0};
-  for (int w = 0; w < 4; ++w)
-    for (int i = 0; i < 4; ++i)
-      if (4 * w + i < valid) v[w] |= (int)((uint32_t)(uint8_t)p[4 * w + i] << (8 * i));
+  if (at + 16 <= dim) return load_bytes(row + at);
+  if (at >= dim) return v;
+  if (dim >= 16) {
+    const unsigned __int128 last = __builtin_bit_cast(unsigned __int128, load_bytes(row + dim - 16));
+    return __builtin_bit_cast(Bytes16, last >> (8 * (at + 16 - dim)));
+  }
+#pragma unroll 1
+  for (int i = 0; i < dim; ++i) {                            // (a row of fewer than 16 bytes: at is 0)
+    const int b = (int)((uint32_t)(uint8_t)row[i] << (8 * (i & 3)));
+    v[0] |= i >> 2 == 0 ? b : 0;
+    v[1] |= i >> 2 == 1 ? b : 0;
+    v[2] |= i >> 2 == 2 ? b : 0;
+    v[3] |= i >> 2 == 3 ? b : 0;
+  }
   return v;
 }
 
-// kMt x kVt tiles of 32 x 32 a wave (tokens x vocabulary), kWm x kWv waves.  With kDirect rows begin at multiples of 16 bytes and go
-// from memory into shared memory by themselves (all but a last step whose bytes are no multiple of 16); else through registers.
-template <typename T, int kMt, int kVt, int kWm, int kWv, int kStages, bool kDirect>
+// Where a row ends within 16 bytes or before them, its last 16 are taken instead, of tokens and weights alike; of the tokens' those are
+// cleared that the 16 before them have as well: the mask of a word of them.
+__device__ inline int keeps(int cleared, int word) {
+  const int bytes = cleared - 4 * word;
+  return bytes >= 4 ? 0 : bytes <= 0 ? -1 : -1 << (8 * bytes);
+}
+
+// kMt x kVt tiles of 32 x 32 a wave (tokens x vocabulary), kWm x kWv waves; kStages stages of kStep bytes of each row.  With kDirect rows
+// begin at multiples of 4 bytes and have a multiple of 4, at least 16, and go from memory into shared memory by themselves; else through
+// registers.  A workgroup has tiles gridDim.x apart, and the stages go on from one to the next: while a tile's logits are written, the
+// next one's first stages are on their way.  (Behind the last tile stages are fetched once more, and not used: the loop has no branches.)
+template <typename T, int kMt, int kVt, int kWm, int kWv, int kStages, int kStep, bool kDirect>
 __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, T* out) {
-  constexpr int kWaves = kWm * kWv, kThreads = 64 * kWaves, kTokens = 32 * kMt * kWm, kWords = 32 * kVt * kWv;
-  constexpr int kRows = kTokens + kWords, kLoads = kRows / 8 / kWaves, kStage = kRows * kStep;
-  static_assert(kRows % (8 * kWaves) == 0 && kTokens % 8 == 0);
-  constexpr int kWidth = Vec<T>::kWidth, kOutRow = kWords * (int)sizeof(T) + 16, kOutBytes = 32 * kWm * kOutRow;
-  __shared__ __attribute__((aligned(16))) int8_t shared[kStages * kStage > kOutBytes ? kStages * kStage : kOutBytes];
-  const Tile tile = tile_of(blockIdx.x, a.token_tiles, a.tiles);
-  const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * kWords;
+  constexpr int kWaves = kWm * kWv, kTokens = 32 * kMt * kWm, kWords = 32 * kVt * kWv;
+  constexpr int kRows = kTokens + kWords, kStage = kRows * kStep;
+  constexpr int kChunks = kStep / 16, kAtOnce = 64 / kChunks, kLoads = kRows / kAtOnce / kWaves;      // chunks of a row; rows of a load
+  constexpr int kParts = kStep / 32, kSets = kDirect ? 2 : 1;      // parts of a step: products of 32 bytes of each row
+  static_assert(kRows % (kAtOnce * kWaves) == 0 && (kStep == 64 || kStep == 128) && (kDirect || kStages == 2));
+  constexpr int kOutTokens = kMt * kVt >= 8 ? 32 : 16;       // whose logits are in a wave's corner at once: what there is room for
+  constexpr int kOutRow = 64 + 16;                           // 64 bytes of a token's logits, and room between rows
+  constexpr int kStores = kMt * kVt * (int)sizeof(T);        // of a tile, by each wave
+  constexpr int kScales = (kRows + 63) / 64 * 64, kScaleSets = kStages + 1;      // (with one step a tile, a wave may be at the one before)
+  // (One array: of several the compiler knows which of them a transfer writes, and has every reading of that wait for it.)
+  __shared__ __attribute__((aligned(16))) int8_t stages[kStages * kStage + kWaves * kOutTokens * kOutRow + kScaleSets * kScales * 4];
+  int8_t* const corners = stages + kStages * kStage;
+  float* const tile_scales = (float*)(corners + kWaves * kOutTokens * kOutRow);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wave_token = wave / kWv * (32 * kMt), wave_word = wave % kWv * (32 * kVt);
+  const int steps = (a.dim + kStep - 1) / kStep, ragged = a.dim % kStep ? steps - 1 : -1;
+  const unsigned mine = (a.tiles - blockIdx.x + gridDim.x - 1) / gridDim.x;
 
-  // Loading: a wave's instruction has eight rows of a stage.  The 16 bytes c of row r lie at place c ^ (r & 7) of the row, so that eight
-  // lanes that read the same columns of eight rows meet all banks once.
-  const int8_t* from[kLoads];
-  const int chunk = (lane & 7) ^ (lane >> 3);
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int row = (wave * kLoads + i) * 8 + (lane >> 3);   // (rows behind the last are the last once more: nobody stores their logits)
-    if (row < kTokens) from[i] = a.q + min(token + row, a.n - 1) * a.q_stride + chunk * 16;
-    else from[i] = a.weight + min(word + row - kTokens, a.vocab - 1) * a.weight_stride + chunk * 16;
-  }
+  // Loading.  The 16 bytes c of row r lie at place c ^ turn(r): shared memory serves sixteen lanes at a time from 64 banks, and so sixteen
+  // rows of the same columns lie in 256 bytes once.
+  // A wave's loads are of tokens or of weights alone.
+  constexpr int kOwn = kRows / kWaves;
+  static_assert(kTokens % kOwn == 0);
+  const bool of_tokens = wave * kOwn < kTokens;
+  const int in_load = lane / kChunks, own_row = wave * kOwn - (of_tokens ? 0 : kTokens) + in_load;
+  const auto place = [&](int i) { return ((lane % kChunks) ^ turn<kStep>(wave * kOwn + i * kAtOnce + in_load)) * 16; };
+  const int8_t* from = nullptr;                              // the tile's first row
+  uint32_t offset[kLoads];                                   // of each load's row and this lane's place in it, from there
   Bytes16 held[kDirect ? 1 : kLoads];
-  const auto fetch = [&](int step) {
-    int8_t* to = shared + step % kStages * kStage + wave * kLoads * 1024;
-    const int left = a.dim - step * kStep - chunk * 16;      // bytes of the row from this lane's on
-    if (a.dim - step * kStep >= kStep) {
+  unsigned fetch_tile = 0;
+  int fetch_step = 0, fetch_stage = 0;
+  const auto begin_fetch = [&] {
+    if (fetch_step > 0 || fetch_tile >= mine) return;
+    const Tile tile = tile_of(blockIdx.x + fetch_tile * gridDim.x, a.token_tiles, a.tiles);
+    const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * kWords;
+    from = of_tokens ? a.q + token * a.q_stride : a.weight + word * a.weight_stride;
+    const int64_t last = (of_tokens ? a.n - token : a.vocab - word) - 1;
+    const uint32_t stride = (uint32_t)(of_tokens ? a.q_stride : a.weight_stride);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)                         // (rows behind the last: the last once more, nobody stores their logits)
+      offset[i] = (uint32_t)min((int64_t)(own_row + i * kAtOnce), last) * stride + (uint32_t)place(i);
+    for (int i = wave * 64; i < kRows; i += kWaves * 64) {
+      const int row = i + lane;
+      const float* p = row < kTokens ? a.scales + min(token + row, a.n - 1) : a.weight_scales + min(word + row - kTokens, a.vocab - 1);
+      transfer<4>(p, tile_scales + fetch_tile % kScaleSets * kScales + i);
+    }
+  };
+  const auto fetch = [&] {
+    int8_t* to = stages + fetch_stage * kStage + wave * kLoads * 1024;
+    const int8_t* here = from + fetch_step * kStep;
+    if (fetch_step != ragged) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        if constexpr (kDirect)
-          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[i] + step * kStep),
-                                           (__attribute__((address_space(3))) void*)(to + i * 1024), 16, 0, 0);
-        else held[i] = load_bytes(from[i] + step * kStep);
+        if constexpr (kDirect) transfer<16>(here + offset[i], to + i * 1024);
+        else held[i] = load_bytes(here + offset[i]);
       }
     } else {
-      if (kDirect && a.dim % 16 == 0) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          const int8_t* p = left > 0 ? from[i] + step * kStep : (const int8_t*)kZeros;
-          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                           (__attribute__((address_space(3))) void*)(to + i * 1024), 16, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          const Bytes16 v = load_some_bytes(from[i] + step * kStep, left);
-          if constexpr (kDirect) *(Bytes16*)(to + i * 1024 + lane * 16) = v;
-          else held[i] = v;
-        }
+      for (int i = 0; i < kLoads; ++i) {
+        const int at = fetch_step * kStep + place(i);
+        if constexpr (kDirect) transfer<16>(from + (offset[i] - (uint32_t)place(i) + (uint32_t)min(at, a.dim - 16)), to + i * 1024);
+        else held[i] = load_end(from + (offset[i] - (uint32_t)place(i)), at, a.dim);
+        if constexpr (!kDirect) __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
-  const auto commit = [&](int step) {
+  const auto end_fetch = [&] {
+    if (++fetch_step == steps) {
+      fetch_step = 0;
+      ++fetch_tile;
+    }
+    fetch_stage = fetch_stage + 1 == kStages ? 0 : fetch_stage + 1;
+  };
+  const auto commit = [&](int stage) {
     if constexpr (!kDirect) {
-      int8_t* to = shared + step % kStages * kStage + wave * kLoads * 1024 + lane * 16;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) *(Bytes16*)(to + i * 1024) = held[i];
+      for (int i = 0; i < kLoads; ++i) *(Bytes16*)(stages + stage * kStage + (wave * kLoads + i) * 1024 + lane * 16) = held[i];
     }
   };
 
@@ -131,88 +188,137 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
 #pragma unroll
     for (int v = 0; v < kVt; ++v) sums[m][v] = Sums{};
 
-  const int steps = (a.dim + kStep - 1) / kStep;
+  // The operands of a part, in two sets in turn (where registers have room): while one is multiplied, the next is read, also over the
+  // end of a stage.
   const int row = lane & 31, half = lane >> 5;
+  Bytes16 x[kSets][kMt], w[kSets][kVt];
+  const auto read = [&](int stage, int part) {
+    const int8_t* here = stages + stage * kStage + row * kStep + ((2 * part + half) ^ turn<kStep>(row)) * 16;
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s)
-    if (s < steps) {
-      fetch(s);
-      commit(s);
-    }
-  for (int step = 0; step < steps; ++step) {
-    if (!kDirect || kStages == 2 || step + kStages - 2 >= steps) wait_and_meet<0>();
-    else wait_and_meet<(kStages - 2) * kLoads>();
-    const bool more = step + kStages - 1 < steps;
-    if (more) fetch(step + kStages - 1);
-    const int8_t* stage = shared + step % kStages * kStage;
-    const int8_t *tokens = stage + (wave_token + row) * kStep, *words = stage + (kTokens + wave_word + row) * kStep;
+    for (int v = 0; v < kVt; ++v) w[part % kSets][v] = *(const Bytes16*)(here + (kTokens + wave_word + v * 32) * kStep);
 #pragma unroll
-    for (int k = 0; k < kStep / 32; ++k) {
-      const int at = ((2 * k + half) ^ (lane & 7)) * 16;
-      Bytes16 t[kMt], w[kVt];
-#pragma unroll
-      for (int m = 0; m < kMt; ++m) t[m] = *(const Bytes16*)(tokens + m * 32 * kStep + at);
-#pragma unroll
-      for (int v = 0; v < kVt; ++v) w[v] = *(const Bytes16*)(words + v * 32 * kStep + at);
-#pragma unroll
-      for (int m = 0; m < kMt; ++m)
-#pragma unroll
-        for (int v = 0; v < kVt; ++v) sums[m][v] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[v], t[m], sums[m][v], 0, 0, 0);
-    }
-    if (more) commit(step + kStages - 1);
-  }
+    for (int m = 0; m < kMt; ++m) x[part % kSets][m] = *(const Bytes16*)(here + (wave_token + m * 32) * kStep);
+  };
 
-  // Element 4 g + j of sums: vocabulary 8 g + 4 half + j, token `row` of the tile of 32 x 32.
-  float word_scale[kVt][16];
-#pragma unroll
-  for (int v = 0; v < kVt; ++v)
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      word_scale[v][i] = a.weight_scales[min(word + wave_word + 32 * v + 8 * (i / 4) + 4 * half + i % 4, a.vocab - 1)];
-  const int columns = (int)min((int64_t)kWords, a.vocab - word);
-#pragma unroll
-  for (int m = 0; m < kMt; ++m) {
-    const float scale = a.scales[min(token + wave_token + 32 * m + row, a.n - 1)];
-    __syncthreads();
-    int8_t* to = shared + (wave / kWv * 32 + row) * kOutRow;
-#pragma unroll
-    for (int v = 0; v < kVt; ++v) {
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        T* p = (T*)to + wave_word + 32 * v + 8 * g + 4 * half;
-        float x[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = (float)sums[m][v][4 * g + j] * scale * word_scale[v][4 * g + j];
-        if constexpr (sizeof(T) == 4) {
-          *(Words*)p = Vec<float>::of(x).w;
-        } else {
-          typedef T Four __attribute__((ext_vector_type(4)));
-          *(Four*)p = Four{from_float<T>(x[0]), from_float<T>(x[1]), from_float<T>(x[2]), from_float<T>(x[3])};
-        }
-      }
-    }
-    __syncthreads();
-    constexpr int kVecs = kWords / kWidth, kAtOnce = kThreads / kVecs;
-    static_assert(kThreads % kVecs == 0);
-    const int column = threadIdx.x % kVecs * kWidth;
-#pragma unroll
-    for (int r = 0; r < 32 * kWm; r += kAtOnce) {
-      const int here = r + (int)threadIdx.x / kVecs;
-      const int64_t t = token + here / 32 * (32 * kMt) + 32 * m + here % 32;
-      if (here < 32 * kWm && t < a.n && column < columns) {
-        Vec<T> v;
-        v.w = *(const Words*)(shared + here * kOutRow + column * (int)sizeof(T));
-        T* p = out + t * a.out_stride + word + column;
-        if (column + kWidth <= columns) v.store(p);
-        else {
-          float x[kWidth];
-          v.get(x);
-          for (int i = 0; i < kWidth; ++i)
-            if (column + i < columns) p[i] = from_float<T>(x[i]);
-        }
-      }
-    }
+#pragma unroll 1
+  for (int s = 0; s < kStages - 1; ++s) {
+    begin_fetch();
+    fetch();
+    commit(s);
+    end_fetch();
   }
+  if constexpr (kDirect) {
+    wait_and_meet<(kStages - 2) * kLoads>();
+    read(0, 0);
+  } else {
+    wait_and_meet<0>();
+  }
+  int stage = 0, stored = 0;                                 // stored: of how many steps to come the stages are older than a whole tile's stores
+  for (unsigned t = 0; t < mine; ++t) {
+    const Tile tile = tile_of(blockIdx.x + t * gridDim.x, a.token_tiles, a.tiles);
+    const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * kWords;
+#pragma unroll 1
+    for (int step = 0; step < steps; ++step) {
+      begin_fetch();
+      const int next = stage + 1 == kStages ? 0 : stage + 1;
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+        if (kDirect && part + 1 < kParts) {
+          read(stage, part + 1);
+        } else if (kDirect) {
+          // The next stage has come when all but the later ones' transfers have ended, and a tile's stores that came after those.
+          end_fetch();
+          if (kStages == 2) wait_and_meet<0>();
+          else if (stored > 0) wait_and_meet<(kStages - 2) * kLoads + kStores>();
+          else wait_and_meet<(kStages - 2) * kLoads>();
+          stored = stored > 0 ? stored - 1 : 0;
+          read(next, 0);
+        } else {
+          read(stage, part);
+        }
+        if (part == 0) fetch();
+        __builtin_amdgcn_sched_barrier(0);
+        if (kDirect && step == ragged) {                     // (nowhere, where rows fill their last step)
+          const int cleared = step * kStep + (2 * part + half) * 16 + 16 - a.dim;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int m = 0; m < kMt; ++m) x[part % kSets][m][i] &= keeps(cleared, i);
+        }
+#pragma unroll
+        for (int m = 0; m < kMt; ++m)
+#pragma unroll
+          for (int v = 0; v < kVt; ++v) sums[m][v] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[part % kSets][v], x[part % kSets][m], sums[m][v], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (!kDirect) {
+        commit(next);
+        end_fetch();
+        wait_and_meet<0>();
+      }
+      stage = next;
+    }
+
+    // Element 4 g + j of sums: vocabulary 8 g + 4 half + j, token `row` of 32 x 32.  A wave's logits go through a corner of shared
+    // memory of its own, 64 bytes of some tokens at a time; its accesses are in order by themselves.
+    const float* scales = tile_scales + t % kScaleSets * kScales;
+    int8_t* corner = corners + wave * kOutTokens * kOutRow;
+    const bool whole = token + kTokens <= a.n && word + kWords <= a.vocab;
+    constexpr int kWidth = Vec<T>::kWidth, kEights = 8 / (int)sizeof(T);           // groups of eight words in 64 bytes
+#pragma unroll
+    for (int m = 0; m < kMt; ++m) {
+      const float scale = scales[wave_token + 32 * m + row];
+#pragma unroll
+      for (int first = 0; first < 4 * kVt; first += kEights) {
+#pragma unroll
+        for (int part = 0; part < 32 / kOutTokens; ++part) {
+          if (kOutTokens == 32 || row / kOutTokens == part) {
+#pragma unroll
+            for (int i = 0; i < kEights; ++i) {
+              const int v = (first + i) / 4, g = (first + i) % 4;
+              const Words of = *(const Words*)(scales + kTokens + wave_word + 32 * v + 8 * g + 4 * half);
+              float y[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) y[j] = (float)sums[m][v][4 * g + j] * scale * __uint_as_float(of[j]);
+              T* p = (T*)(corner + row % kOutTokens * kOutRow) + 8 * i + 4 * half;
+              if constexpr (sizeof(T) == 4) {
+                *(Words*)p = Vec<float>::of(y).w;
+              } else {
+                typedef T Four __attribute__((ext_vector_type(4)));
+                *(Four*)p = Four{from_float<T>(y[0]), from_float<T>(y[1]), from_float<T>(y[2]), from_float<T>(y[3])};
+              }
+            }
+          }
+          // (Lanes read what others have written: the compiler is not to keep what a lane has read before.)
+          asm volatile("" ::: "memory");
+#pragma unroll
+          for (int i = 0; i < kOutTokens / 16; ++i) {
+            const int r = lane / 4 + 16 * i, column = wave_word + 8 * first + lane % 4 * kWidth;
+            Vec<T> y;
+            y.w = *(const Words*)(corner + r * kOutRow + lane % 4 * 16);
+            const int64_t to = token + wave_token + 32 * m + kOutTokens * part + r;
+            T* p = out + to * a.out_stride + word + column;
+            if (whole) {
+              y.store(p);
+            } else if (to < a.n) {
+              float z[kWidth];
+              y.get(z);
+              const int64_t left = a.vocab - word - column;
+              if (left >= kWidth) y.store(p);
+              else
+                for (int j = 0; j < kWidth; ++j)
+                  if (j < left) p[j] = from_float<T>(z[j]);
+            }
+          }
+          asm volatile("" ::: "memory");
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < kVt; ++v) sums[m][v] = Sums{};
+    }
+    stored = whole ? kStages - 2 : 0;                        // (stages that were on their way before these stores)
+  }
+  wait_and_meet<0>();                                        // (nothing may come into shared memory when it is another workgroup's)
 }
 
 }  // namespace bpe

@@ -61,6 +61,23 @@ def test_views(n):
             check(n, 270, dim, torch.bfloat16, q_view, weight_view)
 
 
+@pytest.mark.parametrize("dim", [48, 128, 304, 512, 700])
+@pytest.mark.parametrize("n", [5, 32, 33, 64, 100, 200, 290, 520])
+def test_many_tiles_of_a_workgroup(n, dim):
+    """Workgroups go from one tile to the next with stages on their way: every logit, several times, of one, two and more steps."""
+    import paper_2507_11941_amd as bpe
+
+    vocab = 100260 if n < 128 else 70001
+    q, weight, scales = bytes_of(n, dim, 1), bytes_of(vocab, dim, 2), scales_of(n, 3)
+    weight_scales = scales_of(vocab, 4)
+    sums = q.double() @ weight.double().t()                  # (whole numbers below 2^53)
+    for dtype in (torch.bfloat16, torch.float32):
+        # what the kernel rounds: the sum, its products with either scale, the result
+        want = (sums.float() * scales[:, None] * weight_scales).to(dtype)
+        for _ in range(4):
+            assert torch.equal(bpe.project_8bit(q, scales, weight, weight_scales, dtype), want)
+
+
 @pytest.mark.parametrize("n", [9, 60, 130])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_nothing_else_is_written(n, dtype):
