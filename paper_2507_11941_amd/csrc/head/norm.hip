@@ -48,7 +48,23 @@ void launch_norm(NormArgs<T, W> a, int64_t n, hipStream_t stream) {
   }
 }
 
-int64_t rows_of_group(int64_t n) { return std::min(kGradRows, std::max<int64_t>(1, (n + 511) / 512)); }
+int64_t rows_of_group(int64_t n) {
+  const int64_t groups = n >= 4096 ? 1024 : 512;
+  return std::min(kGradRows, std::max<int64_t>(1, (n + groups - 1) / groups));
+}
+
+// The same for the gradient, whose threads hold more besides: one vector a lane where there are threads enough.
+template <typename T, typename F>
+bool with_grad_variant(int64_t dim, F&& f) {
+  const int64_t vecs = dim / Vec<T>::kWidth;
+  if (vecs <= 64) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+  else if (vecs <= 128) f(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{});
+  else if (vecs <= 256) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+  else if (vecs <= 512) f(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{});
+  else if (vecs <= 1024) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
+  else return false;
+  return true;
+}
 
 // Arguments that the two forms of the norm share.
 bool is_norm(const void* x, int dtype, int64_t n, int64_t dim, int64_t stride, const void* residual, int64_t residual_stride,
@@ -172,7 +188,7 @@ int bpe_add_norm_grad(const void* grad, int dtype, int64_t n, int64_t dim, int64
     a.dim = (int)dim;
     a.each = (int)each;
     if (n > 0) {
-      const bool held = with_variant<T>(dim, [&](auto threads, auto vecs) {
+      const bool held = with_grad_variant<T>(dim, [&](auto threads, auto vecs) {
         hipLaunchKernelGGL((norm_grad_kernel<T, W, threads.value, vecs.value>), dim3((unsigned)groups), dim3(threads.value), 0, stream, a);
       });
       if (!held) {

@@ -49,23 +49,52 @@ __device__ inline double sum_all(double mine, double* part) {
   return mine;
 }
 
+template <int kThreads>
+__device__ inline double largest_all(double mine, double* part) {
+  for (int d = 32; d >= 1; d >>= 1) mine = fmax(mine, __shfl_xor(mine, d));
+  if constexpr (kThreads > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    mine = part[0];
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) mine = fmax(mine, part[w]);
+  }
+  return mine;
+}
+
 // A row's statistics: its sum of squares, 0 or NaN (NaN where the weights hold an infinity or NaN), and its largest |product|.
+template <typename V>
 struct RowSums {
   float squares, odd;
-  double top;
+  V top;
 };
 
-template <int kThreads, bool kTop>
-__device__ inline RowSums join_sums(RowSums mine) {
+template <bool kExact>
+struct Largest {
+  typedef float Type;
+};
+template <>
+struct Largest<false> {
+  typedef double Type;
+};
+
+__device__ inline float magnitude(float x) { return fabsf(x); }
+__device__ inline double magnitude(double x) { return fabs(x); }
+__device__ inline float larger(float a, float b) { return fmaxf(a, b); }
+__device__ inline double larger(double a, double b) { return fmax(a, b); }
+
+template <int kThreads, bool kTop, typename V>
+__device__ inline RowSums<V> join_sums(RowSums<V> mine) {
   for (int d = 32; d >= 1; d >>= 1) {
     mine.squares += __shfl_xor(mine.squares, d);
     if constexpr (kTop) {
       mine.odd += __shfl_xor(mine.odd, d);
-      mine.top = fmax(mine.top, __shfl_xor(mine.top, d));
+      mine.top = larger(mine.top, __shfl_xor(mine.top, d));
     }
   }
   if constexpr (kThreads > 64) {
-    __shared__ RowSums part[kThreads / 64];
+    __shared__ RowSums<V> part[kThreads / 64];
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
     __syncthreads();
     mine = part[0];
@@ -74,7 +103,7 @@ __device__ inline RowSums join_sums(RowSums mine) {
       mine.squares += part[w].squares;
       if constexpr (kTop) {
         mine.odd += part[w].odd;
-        mine.top = fmax(mine.top, part[w].top);
+        mine.top = larger(mine.top, part[w].top);
       }
     }
   }
@@ -125,21 +154,23 @@ __device__ inline Rounding rounding_of(double top, double root, bool odd, float*
   return r;
 }
 
-// s w 127 / top to the nearest integer.  In 32 bits the quotient is off by at most five roundings of 127, 3.8e-5: only what lies
-// within 1e-4 of the middle between two integers is computed in 64 bits, one vector of eight in six hundred.
-template <int kWidth>
-__device__ inline void to_8bit(const float (&s)[kWidth], const float (&w)[kWidth], const Rounding& r, bool odd, int (&q)[kWidth]) {
+// s w 127 / top to the nearest integer, in the low byte of each number.  In 32 bits the quotient is off by at most three roundings of
+// 127, 2.3e-5: only what lies within 1e-4 of the middle between two integers is computed in 64 bits, one vector of eight in six hundred.
+// (Added to 1.5 x 2^23 a number is rounded to an integer, which the last bits of the sum hold.)
+template <bool kWeights, int kWidth>
+__device__ inline void to_8bit(const float (&s)[kWidth], const float (&w)[kWidth], const Rounding& r, bool odd, uint32_t (&q)[kWidth]) {
+  constexpr float kInteger = 12582912.0f;
   float far = 0.0f;
 #pragma unroll
   for (int i = 0; i < kWidth; ++i) {
-    const float v = s[i] * w[i] * r.factor, near = rintf(v);
-    far = fmaxf(far, fabsf(v - near));
-    q[i] = (int)near;
+    const float p = kWeights ? s[i] * w[i] : s[i], sum = fmaf(p, r.factor, kInteger);
+    far = fmaxf(far, fabsf(fmaf(p, r.factor, kInteger - sum)));
+    q[i] = __float_as_uint(sum);
   }
   if (r.slow || far > 0.4999f) {
 #pragma unroll
     for (int i = 0; i < kWidth; ++i) {
-      q[i] = (int)rint((double)s[i] * (double)w[i] * 127.0 / r.top);
+      q[i] = (uint32_t)(int)rint((double)s[i] * (kWeights ? (double)w[i] : 1.0) * 127.0 / r.top);
       __builtin_amdgcn_sched_barrier(0);                     // (side by side these quotients would take all registers)
     }
   }
@@ -150,28 +181,26 @@ __device__ inline void to_8bit(const float (&s)[kWidth], const float (&w)[kWidth
 }
 
 template <int kWidth>
-__device__ inline void store_8bit(int8_t* p, const int (&q)[kWidth]) {
+__device__ inline void store_8bit(int8_t* p, const uint32_t (&q)[kWidth]) {
   typedef uint32_t Bytes __attribute__((ext_vector_type(kWidth / 4), aligned(1)));
-  uint32_t w[kWidth / 4];
+  Bytes v;
 #pragma unroll
-  for (int i = 0; i < kWidth / 4; ++i)
-    w[i] = (uint32_t)(q[4 * i] & 255) | (uint32_t)(q[4 * i + 1] & 255) << 8 | (uint32_t)(q[4 * i + 2] & 255) << 16 | (uint32_t)q[4 * i + 3] << 24;
-  if constexpr (kWidth == 4) {
-    typedef uint32_t Word __attribute__((aligned(1)));
-    *(Word*)p = w[0];
-  } else {
-    Bytes v;
-#pragma unroll
-    for (int i = 0; i < kWidth / 4; ++i) v[i] = w[i];
-    *(Bytes*)p = v;
+  for (int i = 0; i < kWidth / 4; ++i) {
+    // byte 0 of one number and byte 0 of the other, twice, then the two halves
+    const uint32_t low = __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0c0c0400), high = __builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x0c0c0400);
+    const uint32_t all = low | high << 16;
+    if constexpr (kWidth == 4) v = all;
+    else v[i] = all;
   }
+  *(Bytes*)p = v;
 }
 
 // One workgroup a row, which stays in registers: up to kVecs vectors a lane, and the elements behind whole vectors, one a thread.
 template <typename T, typename W, int kKind, int kThreads, int kVecs>
 __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs<T, W> a) {
   constexpr int kWidth = Vec<T>::kWidth;
-  constexpr bool kEight = kKind != kNorm;
+  // kExact: products of 16-bit numbers have 32 bits at most, so that their largest is found in 32 bits where it is within their range.
+  constexpr bool kEight = kKind != kNorm, kExact = kKind == kRows8 || (sizeof(T) == 2 && sizeof(W) == 2);
   const int64_t t = a.first + blockIdx.x;
   const int tid = threadIdx.x, whole = a.dim / kWidth, rest = a.dim % kWidth, edge_at = whole * kWidth + tid;
   const T* x = a.x + t * a.stride;
@@ -223,7 +252,8 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs<T, W> a) {
     if (tid < rest) summed[edge_at] = from_float<T>(edge);
   }
 
-  RowSums sums{edge * edge, kEight ? edge_w * 0.0f : 0.0f, kEight ? fabs((double)edge * (double)edge_w) : 0.0};
+  typedef typename Largest<kExact>::Type Top;
+  RowSums<Top> sums{edge * edge, kEight ? edge_w * 0.0f : 0.0f, kEight ? magnitude((Top)edge * (Top)edge_w) : (Top)0};
   if constexpr (kKind == kRows8) sums.odd = edge * 0.0f;
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) {
@@ -234,18 +264,20 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs<T, W> a) {
       if constexpr (kKind != kRows8) sums.squares = fmaf(s[i], s[i], sums.squares);
       if constexpr (kEight) {
         sums.odd = fmaf(kKind == kRows8 ? s[i] : w[k][i], 0.0f, sums.odd);
-        sums.top = fmax(sums.top, fabs((double)s[i] * (double)w[k][i]));
+        sums.top = larger(sums.top, magnitude((Top)s[i] * (Top)w[k][i]));
       }
     }
   }
-  const RowSums all = join_sums<kThreads, kEight>(sums);
+  const RowSums<Top> all = join_sums<kThreads, kEight>(sums);
   // (Rows are converted once more: the 64-bit products, kept for where they are needed again, would take most registers.)
   if constexpr (kEight) {
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       asm("" : "+v"(v[k].w));
+      if constexpr (kKind != kRows8) {
 #pragma unroll
-      for (int i = 0; i < kWidth; ++i) asm("" : "+v"(w[k][i]));
+        for (int i = 0; i < kWidth; ++i) asm("" : "+v"(w[k][i]));
+      }
     }
   }
   float root = 1.0f;
@@ -284,24 +316,35 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs<T, W> a) {
     }
     if (tid < rest) out[edge_at] = from_float<T>(edge * root * edge_w);
   } else {
+    double top = all.top;
+    if (kExact && kKind == kNorm8 && !(all.top > 1e-30f && all.top < 1e30f)) {       // (the same for the whole workgroup)
+      __shared__ double part[kThreads / 64];
+      double mine = fabs((double)edge * (double)edge_w);
+      for (int k = 0; k < kVecs; ++k) {
+        float s[kWidth];
+        v[k].get(s);
+        for (int i = 0; i < kWidth; ++i) mine = fmax(mine, fabs((double)s[i] * (double)w[k][i]));
+      }
+      top = largest_all<kThreads>(mine, part);
+    }
     float scale;
-    const Rounding r = rounding_of(all.top, root_64, odd, &scale);
+    const Rounding r = rounding_of(top, root_64, odd, &scale);
     if (tid == 0) a.scales[t] = scale;
     int8_t* q = a.q + t * a.q_stride;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       if (k * kThreads + tid < whole) {
         float s[kWidth];
-        int to[kWidth];
+        uint32_t to[kWidth];
         v[k].get(s);
-        to_8bit<kWidth>(s, w[k], r, odd, to);
+        to_8bit<kKind != kRows8>(s, w[k], r, odd, to);
         store_8bit<kWidth>(q + (k * kThreads + tid) * kWidth, to);
       }
     }
     if (tid < rest) {
       const float s[1] = {edge}, one[1] = {edge_w};
-      int to[1];
-      to_8bit<1>(s, one, r, odd, to);
+      uint32_t to[1];
+      to_8bit<kKind != kRows8>(s, one, r, odd, to);
       q[edge_at] = (int8_t)to[0];
     }
   }
@@ -318,7 +361,7 @@ __global__ void __launch_bounds__(1024) long_norm_kernel(NormArgs<T, W> a) {
   const T* residual = a.residual ? a.residual + t * a.residual_stride : nullptr;
   T* summed = a.residual ? a.summed + t * a.summed_stride : nullptr;
   double squares = 0.0;
-  RowSums sums{0.0f, 0.0f, 0.0};
+  RowSums<double> sums{0.0f, 0.0f, 0.0};
   for (int j = threadIdx.x; j < a.dim; j += kThreads) {
     float s = to_float(x[j]);
     if (residual) {
@@ -333,7 +376,7 @@ __global__ void __launch_bounds__(1024) long_norm_kernel(NormArgs<T, W> a) {
       sums.top = fmax(sums.top, fabs((double)s * (double)w));
     }
   }
-  const RowSums all = join_sums<kThreads, kEight>(sums);
+  const RowSums<double> all = join_sums<kThreads, kEight>(sums);
   bool odd = !(all.odd == 0.0f);
   double root = 1.0;
   if constexpr (kKind != kRows8) {
@@ -353,8 +396,8 @@ __global__ void __launch_bounds__(1024) long_norm_kernel(NormArgs<T, W> a) {
     int8_t* q = a.q + t * a.q_stride;
     for (int j = threadIdx.x; j < a.dim; j += kThreads) {
       const float s[1] = {to_float(from[j])}, w[1] = {kKind == kRows8 ? 1.0f : to_float(a.weight[j])};
-      int to[1];
-      to_8bit<1>(s, w, r, odd, to);
+      uint32_t to[1];
+      to_8bit<true>(s, w, r, odd, to);
       q[j] = (int8_t)to[0];
     }
   }
@@ -388,33 +431,40 @@ __global__ void __launch_bounds__(kThreads) norm_grad_kernel(NormGradArgs<T, W> 
     if (k * kThreads + tid < whole) load_weights<kWidth>(a.weight + (k * kThreads + tid) * kWidth, w[k]);
   }
   if (tid < rest) edge_w = to_float(a.weight[edge_at]);
-  for (int64_t t = begin; t < end; ++t) {
+  // A row's vectors, of which the next row's are on their way while this one's sum is joined.
+  Vec<T> next_g[kVecs], next_s[kVecs], next_more[kVecs];
+  float next_edge_g = 0.0f, next_edge_s = 0.0f, next_edge_more = 0.0f, next_r = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) next_g[k] = next_s[k] = next_more[k] = Vec<T>::all(0.0f);
+  const auto load = [&](int64_t t) {
     const T *grad = a.grad + t * a.grad_stride, *summed = a.summed + t * a.summed_stride;
-    const float r = a.rstd[t];
-    Vec<T> g[kVecs], s[kVecs], more[kVecs];
-    float edge_g = 0.0f, edge_h = 0.0f, edge_more = 0.0f;
+    const T* more = a.grad_summed ? a.grad_summed + t * a.grad_summed_stride : nullptr;
+    next_r = a.rstd[t];
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      g[k] = s[k] = Vec<T>::all(0.0f);
       if (k * kThreads + tid < whole) {
-        g[k] = Vec<T>::load(grad + (k * kThreads + tid) * kWidth);
-        s[k] = Vec<T>::load(summed + (k * kThreads + tid) * kWidth);
+        next_g[k] = Vec<T>::load(grad + (k * kThreads + tid) * kWidth);
+        next_s[k] = Vec<T>::load(summed + (k * kThreads + tid) * kWidth);
+        if (more) next_more[k] = Vec<T>::load(more + (k * kThreads + tid) * kWidth);
       }
     }
     if (tid < rest) {
-      edge_g = to_float(grad[edge_at]);
-      edge_h = to_float(summed[edge_at]) * r;
+      next_edge_g = to_float(grad[edge_at]);
+      next_edge_s = to_float(summed[edge_at]);
+      if (more) next_edge_more = to_float(more[edge_at]);
     }
-    if (a.grad_summed) {
-      const T* from = a.grad_summed + t * a.grad_summed_stride;
+  };
+  load(begin);
+  for (int64_t t = begin; t < end; ++t) {
+    Vec<T> g[kVecs], s[kVecs], more[kVecs];
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k)
-        if (k * kThreads + tid < whole) more[k] = Vec<T>::load(from + (k * kThreads + tid) * kWidth);
-      if (tid < rest) edge_more = to_float(from[edge_at]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < kVecs; ++k) more[k] = Vec<T>::all(0.0f);
+    for (int k = 0; k < kVecs; ++k) {
+      g[k] = next_g[k];
+      s[k] = next_s[k];
+      more[k] = next_more[k];
     }
+    const float r = next_r, edge_g = next_edge_g, edge_h = next_edge_s * r, edge_more = next_edge_more;
+    if (t + 1 < end) load(t + 1);
     float dot = edge_g * edge_w * edge_h;
     edge_total = fmaf(edge_g, edge_h, edge_total);
 #pragma unroll
@@ -486,32 +536,45 @@ __global__ void __launch_bounds__(256) long_norm_partial_kernel(NormGradArgs<T, 
   a.partial[group * a.dim + j] = total;
 }
 
-// The weights' gradient from the groups' parts, added in 64 bits: 64 columns a workgroup, sixteen waves that each have every
-// sixteenth group.
+// The weights' gradient from the groups' parts, added in 64 bits: 64 columns a workgroup, four a lane, and every 64th group for each
+// sixteen lanes, so that a thread's reads are few and side by side.
 template <typename O>
 __global__ void __launch_bounds__(1024) norm_weight_kernel(const float* partial, int64_t groups, int dim, int accumulate, O* grad_weight) {
   __shared__ double part[16][64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t j = (int64_t)blockIdx.x * 64 + lane;
-  double total = 0.0;
-  if (j < dim) {
-    constexpr int kDeep = 8;
-    int64_t i = wave;
-    for (; i + 16 * (kDeep - 1) < groups; i += 16 * kDeep) {
-      float v[kDeep];
+  const int64_t j = (int64_t)blockIdx.x * 64 + lane % 16 * 4;
+  double total[4] = {0.0, 0.0, 0.0, 0.0};
+  constexpr int kDeep = 8;
+  for (int64_t i = wave * 4 + lane / 16; i < groups && j < dim; i += 64 * kDeep) {
+    float v[kDeep][4];
 #pragma unroll
-      for (int k = 0; k < kDeep; ++k) v[k] = partial[(i + 16 * k) * dim + j];
-#pragma unroll
-      for (int k = 0; k < kDeep; ++k) total += (double)v[k];
+    for (int k = 0; k < kDeep; ++k) {
+      const float* p = partial + (i + 64 * k) * dim + j;
+      for (int c = 0; c < 4; ++c) v[k][c] = 0.0f;
+      if (i + 64 * k < groups) {
+        if (j + 4 <= dim) Vec<float>::load(p).get(v[k]);
+        else
+          for (int c = 0; c < 4; ++c)
+            if (j + c < dim) v[k][c] = p[c];
+      }
     }
-    for (; i < groups; i += 16) total += (double)partial[i * dim + j];
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k)
+      for (int c = 0; c < 4; ++c) total[c] += (double)v[k][c];
   }
-  part[wave][lane] = total;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    total[c] += __shfl_xor(total[c], 16);
+    total[c] += __shfl_xor(total[c], 32);
+    if (lane < 16) part[wave][lane * 4 + c] = total[c];
+  }
   __syncthreads();
-  if (wave == 0 && j < dim) {
-    for (int w = 1; w < 16; ++w) total += part[w][lane];
-    if (accumulate) total += (double)to_float(grad_weight[j]);
-    grad_weight[j] = from_float<O>((float)total);
+  const int64_t column = (int64_t)blockIdx.x * 64 + threadIdx.x;
+  if (threadIdx.x < 64 && column < dim) {
+    double sum = part[0][threadIdx.x];
+    for (int w = 1; w < 16; ++w) sum += part[w][threadIdx.x];
+    if (accumulate) sum += (double)to_float(grad_weight[column]);
+    grad_weight[column] = from_float<O>((float)sum);
   }
 }
 
