@@ -11,8 +11,8 @@ Bounds, in units of U = 2^-24 (a rounding to 32 bits is at most U of the value):
   mean two more; the element g w - h m has four roundings of its parts.
 * Gradient of the weights: two roundings a term and at most 256 additions in 32 bits, the rest in 64.
 * An 8-bit product's sum is exact: its conversion and the two scales round once each.
-* Adjusted logits: a quotient or product, presence + frequency c, their difference and a bias: at most one rounding each of values
-  no larger than the sum of the parts' magnitudes.
+* Adjusted logits: a product with the penalty or its rounded reciprocal, presence + frequency c, their difference and a bias: at most one
+  rounding each of values no larger than the sum of the parts' magnitudes.  Their gradient: that product.
 """
 import math
 
@@ -127,4 +127,4 @@ def adjust_grad(grad, logits, ids=None, begin=None, end=None, penalties=None, ma
         p = _rows(penalties or (1.0, 0.0, 0.0) if not isinstance(penalties, torch.Tensor) else penalties, n, 3)[:, :1]
         g = torch.where(counts(vocab, ids, begin, end) > 0, torch.where(logits.cpu().double() > 0, g / p, g * p), g)
     g = torch.where(allowed(n, vocab, mask, state), g, 0.0)
-    return g, U * g.abs()
+    return g, U * g.abs()                            # (the reciprocal's; the product's is the result's own)
