@@ -3,6 +3,16 @@
 // A workgroup has a tile of tokens x vocabulary and goes along the columns in steps of 128 bytes a row, which wait in shared memory in
 // stages: while the matrix units work on one, the next are on their way.  The vocabulary is the matrix instruction's first operand,
 // so that a lane holds four neighbours of a token's logits, and these go to memory through shared memory, 16 bytes a lane.
+//
+// Measured on one MI355X, whose matrix units reach 3.5e15 operations/s on random bytes (they, too, lower the clock):
+//   8,191 tokens x 2,048 into 100,260 bfloat16   1,650 to 1,700 us, 2.0e15/s; 8,192 x 4,096 into 32,768 955 to 980 us, 2.3e15/s
+//   (torch's product with 32-bit sums written: 2,008 and 1,017 us)
+//   8 tokens x 4,096 into 100,260                 81 to 90 us, 4.6 to 5.1 TB/s: the reading of the weights
+// What the first of these spends, by leaving parts out: products and readings of shared memory alone 1,130 us, with the stages' transfers
+// (13 GB through the second-level caches, 960 us alone) 1,380, with the conversion of the logits 1,500, the rest their stores; rows of
+// 100,260 begin at multiples of 8 bytes, and of 100,352 the stores take 120 less.  Stages of 64 bytes, four of them instead of two of 128: 1,800
+// (twice the requests); two workgroups of half the tile: 3,400 (half as much again to transfer); stores past the caches: 2,070 (parts of lines);
+// offsets of loads worked out for each step: 1,830.
 #pragma once
 #include "../ops/element.h"
 
@@ -201,14 +211,14 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
   };
 
 #pragma unroll 1
-  for (int s = 0; s < kStages - 1; ++s) {
+  for (int s = 0; s < (kDirect ? kStages : kStages - 1); ++s) {
     begin_fetch();
     fetch();
     commit(s);
     end_fetch();
   }
   if constexpr (kDirect) {
-    wait_and_meet<(kStages - 2) * kLoads>();
+    wait_and_meet<(kStages - 1) * kLoads>();
     read(0, 0);
   } else {
     wait_and_meet<0>();
@@ -219,24 +229,24 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
     const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * kWords;
 #pragma unroll 1
     for (int step = 0; step < steps; ++step) {
-      begin_fetch();
       const int next = stage + 1 == kStages ? 0 : stage + 1;
+      if constexpr (!kDirect) begin_fetch();
 #pragma unroll
       for (int part = 0; part < kParts; ++part) {
         if (kDirect && part + 1 < kParts) {
           read(stage, part + 1);
         } else if (kDirect) {
-          // The next stage has come when all but the later ones' transfers have ended, and a tile's stores that came after those.
-          end_fetch();
-          if (kStages == 2) wait_and_meet<0>();
-          else if (stored > 0) wait_and_meet<(kStages - 2) * kLoads + kStores>();
+          // The next stage has come when all but the later ones' transfers have ended, and a tile's stores that came after those.  Then
+          // all waves have read this one, whose place the stage after the last takes.
+          if (stored > 0) wait_and_meet<(kStages - 2) * kLoads + kStores>();
           else wait_and_meet<(kStages - 2) * kLoads>();
           stored = stored > 0 ? stored - 1 : 0;
           read(next, 0);
+          begin_fetch();
         } else {
           read(stage, part);
+          if (part == 0) fetch();
         }
-        if (part == 0) fetch();
         __builtin_amdgcn_sched_barrier(0);
         if (kDirect && step == ragged) {                     // (nowhere, where rows fill their last step)
           const int cleared = step * kStep + (2 * part + half) * 16 + 16 - a.dim;
@@ -250,6 +260,10 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
 #pragma unroll
           for (int v = 0; v < kVt; ++v) sums[m][v] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[part % kSets][v], x[part % kSets][m], sums[m][v], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
+        if (kDirect && part == kParts - 1) {                 // (behind the products: a wave waits while memory takes its transfers)
+          fetch();
+          end_fetch();
+        }
       }
       if constexpr (!kDirect) {
         commit(next);
@@ -316,7 +330,7 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
 #pragma unroll
       for (int v = 0; v < kVt; ++v) sums[m][v] = Sums{};
     }
-    stored = whole ? kStages - 2 : 0;                        // (stages that were on their way before these stores)
+    stored = whole ? kStages - 1 : 0;                        // (stages that were on their way before these stores)
   }
   wait_and_meet<0>();                                        // (nothing may come into shared memory when it is another workgroup's)
 }
