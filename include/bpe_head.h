@@ -21,7 +21,8 @@ extern "C" {
 /* summed[t] = x[t] + residual[t], rounded to the type; the norm is of that, or of x itself without a residual:
  *   s = summed[t],  rstd[t] = 1 / sqrt(mean over j of s_j^2 + eps),  out[t][j] = s_j * rstd[t] * weight[j].
  *   x, residual, summed, out   [n][dim] of `dtype`; residual and summed may both be NULL.  summed may be x or the residual, and out
- *                              x or the residual (same pointer and stride); else nothing that is written overlaps anything.
+ *                              x or the residual, but not summed (same pointer and stride); else nothing that is written overlaps
+ *                              anything.
  *   weight  [dim] of weight_dtype: BPE_F32 or `dtype`;  rstd float[n], or NULL.
  *   eps     >= 0.  A row of zeros with eps = 0 gives NaN, as do infinities and NaN in a row. */
 int bpe_add_norm(const void* x, int dtype, int64_t n, int64_t dim, int64_t stride, const void* residual, int64_t residual_stride,
@@ -70,17 +71,18 @@ int bpe_project_8bit(const int8_t* q, int64_t n, int64_t dim, int64_t q_stride, 
  * to be 0 and n_ids; ids outside [0, vocab) are padding and count nowhere): a packed batch's string with offsets and offsets + 1,
  * what is before a position with its string's offset and the position, a row of a buffer with its beginning and its length so far.
  * For x = logits[t][v], c the number of times that v is in the history, in this order:
- *   c > 0:  x = x > 0 ? x / repetition : x * repetition;  x = x - (presence + frequency * c)
+ *   c > 0:  x = x > 0 ? x / repetition : x * repetition;  x = x - (presence + frequency * c)      (divided by the rounded reciprocal)
  *   v is bias_ids[i] for an i in bias_begin[t] .. bias_end[t] - 1:  x = x + bias_values[i]; of several such i the last one counts
  *   bit v % 32 of mask[state[t]][v / 32] is 0:  x = -infinity, whatever it was.
  *   penalties   float[n][3]: repetition (> 0), presence and frequency of each row; or NULL: those given for all rows.
- *   ids         int32[n_ids]; begin, end int64[n].  begin and end may be NULL: no history.
+ *   ids         int32[n_ids]; begin, end int64[n].  begin and end may be NULL: no history.  (Of a history or a list of biases the first
+ *               0xfffffff0 are looked at.)
  *   bias_ids, bias_values   int32 and float [n_biases]; bias_begin, bias_end int64[n], bounds as above; both may be NULL: no biases.
  *   mask        int32 [states][mask_stride], mask_stride >= (vocab + 31) / 32 words; or NULL: none.
  *   state       int32[n], each row's mask; a row whose state is outside [0, states) has none.  NULL: row t has mask t (states = n), or
  *               all have the only one (states = 1).
- *   out         [n][vocab] of `dtype`; may be the logits (same pointer and stride), else overlaps nothing.  In place only elements
- *               that change are written, and only those and their neighbours are read.
+ *   out         [n][vocab] of `dtype`; may be the logits (same pointer and stride), else overlaps nothing.  In place only stretches of
+ *               16 bytes in which something changes are written, and read.
  * A mask may leave nothing of a row: it is -infinity throughout. */
 int bpe_adjust_logits(const void* logits, int dtype, int64_t n, int64_t vocab, int64_t stride, const int32_t* ids, int64_t n_ids,
                       const int64_t* begin, const int64_t* end, const float* penalties, float repetition, float presence,

@@ -1,7 +1,10 @@
 """ctypes binding of include/bpe_head.h, the operators at a model's output end: argument marshalling only.
 
 Streams, allocation, strides and refusals are as in ``_ops.py``.  ``add_norm`` and ``adjust_logits`` are recorded by torch's automatic
-differentiation where what they are given wants a gradient; what is in 8 bits carries none, and is refused for a tensor that wants one."""
+differentiation where what they are given wants a gradient; what is in 8 bits carries none, and is refused for a tensor that wants one.
+(A training step that is captured in a graph takes its gradients from ``add_norm_grad`` and ``adjust_logits_grad``, or from
+``torch.autograd.grad``: torch's ``backward()`` adds them up on the stream on which a parameter was first used, which need not be the one
+that is captured.)"""
 from __future__ import annotations
 
 import ctypes
@@ -242,6 +245,7 @@ def project_8bit(q, scales, weight, weight_scales, dtype=None, out=None, stream=
     if stream is not None:
         return _on(stream, project_8bit, q, scales, weight, weight_scales, dtype, out)
     lib = _lib or _load()
+    _no_gradient("project_8bit", scales, weight_scales)
     stride, dev = _bytes(q, "q"), q.device
     n, dim = q.shape
     weight_stride = _bytes(weight, "weight", dev, dim)

@@ -15,11 +15,18 @@ namespace {
 constexpr int64_t kMostRows = (int64_t)1 << 21;             // workgroups of a launch
 constexpr int64_t kGradRows = 256;                          // rows that are summed in 32 bits, at most
 
+// Fewer rows than these have more threads, each with one vector.  One wave a row, and four, us (8 bits, the type, rows to 8 bits; in a graph):
+// 61 rows of 2,048 bfloat16 5.3, 4.1, 3.9 and 3.7, 3.1, 3.1; 500 6.3, 4.6, 4.3 and 4.4, 3.6, 3.5; 1,000 6.6, 5.2, 4.3 and 5.6, 4.5, 4.4; 2,000
+// 8.2, 7.0, 5.7 and 8.0, 6.6, 6.1; 4,000 13.3, 12.0, 8.4 and 14.7, 13.1, 9.6; of 700 columns 500 5.1, 4.0, 3.6 and 4.2, 3.4, 3.4, 2,000 6.2,
+// 5.1, 4.4 and 6.5, 5.0, 5.1.
+constexpr int64_t kFewRows = 1000;
+
 // Calls f with the threads and vectors a lane of the smallest variant whose registers hold a row, or returns false.
 template <typename T, typename F>
-bool with_variant(int64_t dim, F&& f) {
+bool with_variant(int64_t n, int64_t dim, F&& f) {
   const int64_t vecs = dim / Vec<T>::kWidth;
   if (vecs <= 64) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+  else if (vecs <= 256 && n < kFewRows) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
   else if (vecs <= 64 * 4) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
   else if (vecs <= 256 * 2) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
   else if (vecs <= 256 * 4) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
@@ -41,7 +48,7 @@ template <int kKind, typename T, typename W>
 void launch_norm(NormArgs<T, W> a, int64_t n, hipStream_t stream) {
   for (a.first = 0; a.first < n; a.first += kMostRows) {
     const dim3 grid((unsigned)std::min(kMostRows, n - a.first));
-    const bool held = with_variant<T>(a.dim, [&](auto threads, auto vecs) {
+    const bool held = with_variant<T>(n, a.dim, [&](auto threads, auto vecs) {
       hipLaunchKernelGGL((norm_kernel<T, W, kKind, threads.value, vecs.value>), grid, dim3(threads.value), 0, stream, a);
     });
     if (!held) hipLaunchKernelGGL((long_norm_kernel<T, W, kKind>), grid, dim3(1024), 0, stream, a);
@@ -102,7 +109,7 @@ int bpe_add_norm(const void* x, int dtype, int64_t n, int64_t dim, int64_t strid
                  const void* weight, int weight_dtype, float eps, void* summed, int64_t summed_stride, float* rstd, void* out,
                  int64_t out_stride, void* stream) {
   if (!is_norm(x, dtype, n, dim, stride, residual, residual_stride, weight, weight_dtype, eps, summed, summed_stride) ||
-      !aligned(rstd, 4) || !is_matrix(out, dtype, n, dim, out_stride))
+      !aligned(rstd, 4) || !is_matrix(out, dtype, n, dim, out_stride) || (summed && out == summed && n > 0))
     return BPE_EINVAL;
   with_types(dtype, weight_dtype, [&](auto type, auto weight_type) {
     using T = decltype(type);

@@ -32,14 +32,14 @@ def call(name, good, bad):
 
 
 nan, inf = float("nan"), float("inf")
-NORM = dict(x=A, dtype=1, n=4, dim=7, stride=7, residual=A, residual_stride=7, weight=A, weight_dtype=0, eps=1e-6, summed=A, summed_stride=7)
+NORM = dict(x=A, dtype=1, n=4, dim=7, stride=7, residual=A, residual_stride=7, weight=A, weight_dtype=0, eps=1e-6, summed=A + 4096, summed_stride=7)
 BAD_NORM = [("x", None), ("x", A + 1), ("dtype", 3), ("dtype", -1), ("n", -1), ("n", BIG), ("dim", 0), ("dim", BIG), ("stride", 6), ("stride", BIG),
             ("residual", None), ("residual", A + 1), ("residual_stride", 6), ("weight", None), ("weight", A + 2), ("weight_dtype", 2),
             ("weight_dtype", 5), ("eps", -1.0), ("eps", nan), ("eps", inf), ("summed", None), ("summed", A + 1), ("summed_stride", 6)]
 
 
 def test_norm_arguments():
-    call("add_norm", dict(NORM, rstd=A, out=A, out_stride=7, stream=None), [*BAD_NORM, ("rstd", A + 2), ("out", None), ("out", A + 1), ("out_stride", 6)])
+    call("add_norm", dict(NORM, rstd=A, out=A, out_stride=7, stream=None), [*BAD_NORM, ("rstd", A + 2), ("out", None), ("out", A + 1), ("out", A + 4096), ("out_stride", 6)])
     call("add_norm_8bit", dict(NORM, q=A, q_stride=7, scales=A, stream=None),
          [*BAD_NORM, ("q", None), ("q_stride", 6), ("q_stride", BIG), ("scales", None), ("scales", A + 2)])
     call("quantize_rows", dict(x=A, dtype=1, n=4, dim=7, stride=7, q=A, q_stride=7, scales=A, stream=None),
