@@ -211,8 +211,10 @@ int bpe_add_norm_grad(const void* grad, int dtype, int64_t n, int64_t dim, int64
     if (grad_weight) {
       const auto join = [&](auto out_type) {
         using O = decltype(out_type);
-        hipLaunchKernelGGL(norm_weight_kernel<O>, dim3(blocks(dim, 64)), dim3(1024), 0, stream, a.partial, groups, (int)dim, accumulate,
-                           (O*)grad_weight);
+        const unsigned columns = blocks(dim, 64);
+        for (unsigned first = 0; first < columns; first += (unsigned)kMostRows)
+          hipLaunchKernelGGL(norm_weight_kernel<O>, dim3(std::min((unsigned)kMostRows, columns - first)), dim3(1024), 0, stream, a.partial, groups,
+                             (int)dim, accumulate, first, (O*)grad_weight);
       };
       if (grad_weight_dtype == BPE_F32) join(float{});
       else join(type);

@@ -539,10 +539,10 @@ __global__ void __launch_bounds__(256) long_norm_partial_kernel(NormGradArgs<T, 
 // The weights' gradient from the groups' parts, added in 64 bits: 64 columns a workgroup, four a lane, and every 64th group for each
 // sixteen lanes, so that a thread's reads are few and side by side.
 template <typename O>
-__global__ void __launch_bounds__(1024) norm_weight_kernel(const float* partial, int64_t groups, int dim, int accumulate, O* grad_weight) {
+__global__ void __launch_bounds__(1024) norm_weight_kernel(const float* partial, int64_t groups, int dim, int accumulate, unsigned first, O* grad_weight) {
   __shared__ double part[16][64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t j = (int64_t)blockIdx.x * 64 + lane % 16 * 4;
+  const int64_t begin = ((int64_t)first + blockIdx.x) * 64, j = begin + lane % 16 * 4;
   double total[4] = {0.0, 0.0, 0.0, 0.0};
   constexpr int kDeep = 8;
   for (int64_t i = wave * 4 + lane / 16; i < groups && j < dim; i += 64 * kDeep) {
@@ -569,7 +569,7 @@ __global__ void __launch_bounds__(1024) norm_weight_kernel(const float* partial,
     if (lane < 16) part[wave][lane * 4 + c] = total[c];
   }
   __syncthreads();
-  const int64_t column = (int64_t)blockIdx.x * 64 + threadIdx.x;
+  const int64_t column = begin + threadIdx.x;
   if (threadIdx.x < 64 && column < dim) {
     double sum = part[0][threadIdx.x];
     for (int w = 1; w < 16; ++w) sum += part[w][threadIdx.x];

@@ -175,6 +175,25 @@ def test_gradients(dtype, weight_dtype):
         assert_near(in_place, to_x, off, "in place of the sum's gradient")
 
 
+def test_gradient_of_very_many_weights():
+    """More columns than one launch has workgroups for: the weights' gradient about the borders of the launches that join it."""
+    import paper_2507_11941_amd as bpe
+
+    dim = 2 ** 28 + 65
+    g = torch.arange(dim, dtype=torch.int32, device=dev()).remainder_(251).sub_(125).to(torch.bfloat16).view(1, dim)
+    s = torch.arange(dim, dtype=torch.int32, device=dev()).remainder_(241).sub_(120).to(torch.bfloat16).view(1, dim)
+    weight = torch.ones(dim, dtype=torch.bfloat16, device=dev())
+    rstd = torch.full((1,), 0.0078125, device=dev())
+    for accumulate in (False, True):
+        total = torch.full((dim,), 3.0, device=dev())
+        bpe.add_norm_grad(g, s, weight, rstd, out_weight=total, accumulate=accumulate)
+        for begin in (0, 2 ** 27 - 70, 2 ** 28 - 70, dim - 70):
+            some = slice(begin, begin + 70)
+            # (products of two integers of at most 7 bits and a power of two, and 3 more: exact in 32 bits)
+            want = g[0, some].double() * s[0, some].double() * 0.0078125 + (3.0 if accumulate else 0.0)
+            assert torch.equal(total[some].double(), want), (accumulate, begin)
+
+
 def test_gradients_against_differences():
     """The formula's gradient in 64 bits, which the kernels' is compared with, against differences of the norm's formula."""
     g, x, w = (matrix(3, 17, torch.float32, seed).cpu().double() for seed in (1, 2, 3))
