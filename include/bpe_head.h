@@ -59,7 +59,7 @@ int bpe_quantize_rows(const void* x, int dtype, int64_t n, int64_t dim, int64_t 
  *   q       int8 [n][dim], dim <= BPE_MAX_DIM_8BIT (the sum fits 32 bits);  scales float[n]
  *   weight  int8 [vocab][dim];  weight_scales float[vocab]
  *           both with a stride of at most BPE_MAX_STRIDE_8BIT
- *   out     [n][vocab] of `dtype`, overlapping nothing.
+ *   out     [n][vocab] of `dtype`, overlapping nothing; n * vocab <= 10^13.
  * Rows that begin at multiples of 4 bytes and have a multiple of 4 columns are read fastest, at multiples of 128 bytes more so. */
 #define BPE_MAX_DIM_8BIT 131071
 #define BPE_MAX_STRIDE_8BIT 0xfffffe
