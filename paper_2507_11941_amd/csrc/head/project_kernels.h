@@ -5,10 +5,10 @@
 // so that a lane holds four neighbours of a token's logits, and these go to memory through shared memory, 16 bytes a lane.
 //
 // Measured on one MI355X, whose matrix units reach 3.5e15 operations/s on random bytes (they, too, lower the clock):
-//   8,191 tokens x 2,048 into 100,260 bfloat16   1,650 to 1,700 us, 2.0e15/s; 8,192 x 4,096 into 32,768 955 to 980 us, 2.3e15/s
+//   8,191 tokens x 2,048 into 100,260 bfloat16   1,620 to 1,680 us, 2.0e15/s; 8,192 x 4,096 into 32,768 940 to 980 us, 2.3e15/s
 //   (torch's product with 32-bit sums written: 2,008 and 1,017 us)
-//   8 tokens x 4,096 into 100,260                 81 to 90 us, 4.6 to 5.1 TB/s: the reading of the weights
-// What the first of these spends, by leaving parts out: products and readings of shared memory alone 1,130 us, with the stages' transfers
+//   8 tokens x 4,096 into 100,260                 75 to 79 us, 5.2 to 5.5 TB/s: the reading of the weights
+// What the first of these spent at 1,700, by leaving parts out: products and readings of shared memory alone 1,130 us, with the stages' transfers
 // (13 GB through the second-level caches, 960 us alone) 1,380, with the conversion of the logits 1,500, the rest their stores; rows of
 // 100,260 begin at multiples of 8 bytes, and of 100,352 the stores take 120 less.  Stages of 64 bytes, four of them instead of two of 128: 1,800
 // (twice the requests); two workgroups of half the tile: 3,400 (half as much again to transfer); stores past the caches: 2,070 (parts of lines);
@@ -129,6 +129,12 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
   const int wave_token = wave / kWv * (32 * kMt), wave_word = wave % kWv * (32 * kVt);
   const int steps = (a.dim + kStep - 1) / kStep, ragged = a.dim % kStep ? steps - 1 : -1;
   const unsigned mine = (a.tiles - blockIdx.x + gridDim.x - 1) / gridDim.x;
+  // Workgroups begin at different columns, by thirty-seconds of a row, and go round: all at the same columns of rows of 4,096 bytes would
+  // ask the same parts of memory at once.  8 tokens x 4,096 into 100,260: 84 us -> 76; 32 x 8,192 into 50,000: 94 -> 84; 4,096 x 4,096 into
+  // 65,536: 993 -> 960; 8,191 x 2,048 into 100,260: 1,680 -> 1,630.  (Small tiles with the large ones' places 76, 87; large ones with the
+  // small ones' 980, 1,650.)
+  const unsigned die = blockIdx.x % kXcds, begin = kMt * kVt >= 8 ? die * 4 + blockIdx.x / kXcds % 4 : die % 4 * 8;
+  const int first_step = (int)(begin * (unsigned)steps / 32);
 
   // Loading.  The 16 bytes c of row r lie at place c ^ turn(r): shared memory serves sixteen lanes at a time from 64 banks, and so sixteen
   // rows of the same columns lie in 256 bytes once.
@@ -142,9 +148,9 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
   uint32_t offset[kLoads];                                   // of each load's row and this lane's place in it, from there
   Bytes16 held[kDirect ? 1 : kLoads];
   unsigned fetch_tile = 0;
-  int fetch_step = 0, fetch_stage = 0;
+  int fetch_step = first_step, fetch_stage = 0;
   const auto begin_fetch = [&] {
-    if (fetch_step > 0 || fetch_tile >= mine) return;
+    if (fetch_step != first_step || fetch_tile >= mine) return;
     const Tile tile = tile_of(blockIdx.x + fetch_tile * gridDim.x, a.token_tiles, a.tiles);
     const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * kWords;
     from = of_tokens ? a.q + token * a.q_stride : a.weight + word * a.weight_stride;
@@ -179,10 +185,8 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
     }
   };
   const auto end_fetch = [&] {
-    if (++fetch_step == steps) {
-      fetch_step = 0;
-      ++fetch_tile;
-    }
+    if (++fetch_step == steps) fetch_step = 0;
+    if (fetch_step == first_step) ++fetch_tile;
     fetch_stage = fetch_stage + 1 == kStages ? 0 : fetch_stage + 1;
   };
   const auto commit = [&](int stage) {
@@ -228,7 +232,7 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
     const Tile tile = tile_of(blockIdx.x + t * gridDim.x, a.token_tiles, a.tiles);
     const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * kWords;
 #pragma unroll 1
-    for (int step = 0; step < steps; ++step) {
+    for (int count = 0, step = first_step; count < steps; ++count, step = step + 1 == steps ? 0 : step + 1) {
       const int next = stage + 1 == kStages ? 0 : stage + 1;
       if constexpr (!kDirect) begin_fetch();
 #pragma unroll
