@@ -13,12 +13,12 @@ using namespace bpe;
 namespace {
 
 // Tiles of tokens x vocabulary: by eight waves, one workgroup on a compute unit (256 x 256); by eight, two (128 x 128); by four, two
-// (64 x 64).
-enum Size { kLarge, kMiddle, kSmall };
+// (64 x 64); and by four, two (32 x 128), for few tokens.
+enum Size { kLarge, kMiddle, kSmall, kFew };
 
 constexpr struct {
   int tokens, words, at_once;
-} kSizes[] = {{256, 256, 256}, {128, 128, 512}, {64, 64, 512}};
+} kSizes[] = {{256, 256, 256}, {128, 128, 512}, {64, 64, 512}, {32, 128, 512}};
 
 int64_t tiles_of(Size size, int64_t n, int64_t vocab) {
   return (n + kSizes[size].tokens - 1) / kSizes[size].tokens * ((vocab + kSizes[size].words - 1) / kSizes[size].words);
@@ -33,6 +33,10 @@ double rounds_of(Size size, int64_t n, int64_t vocab) {
 }
 
 Size size_of_tiles(int64_t n, int64_t vocab) {
+  // (Tiles for few tokens where some compute unit would have two small ones.  Small and few, us: 8 tokens of 2,048 columns into 16,384 9.5, 9.7,
+  // 20,480 11.7, 9.7, 32,000 13.0, 12.2; of 4,096 into 16,384 15.1, 15.6, 65,536 42.0, 40.8, 100,260 75.7, 76.7; of 768 into 50,257 11.9, 8.5;
+  // 32 of 8,192 into 50,000 84, 75; 20 of 4,097 into 60,000 64, 40.)
+  if (n <= 32 && tiles_of(kSmall, n, vocab) > 256) return kFew;
   if (n <= 64) return kSmall;
   Size best = kLarge;
   for (Size size : {kMiddle, kSmall})
@@ -46,6 +50,15 @@ void launch_tiles(ProjectArgs a, bool direct, T* out, hipStream_t stream) {
   static_assert(kSizes[kSize].tokens == 32 * kMt * kWm && kSizes[kSize].words == 32 * kVt * kWv);
   a.token_tiles = blocks(a.n, kSizes[kSize].tokens);
   a.tiles = (unsigned)tiles_of(kSize, a.n, a.vocab);
+  // For few tokens a tile has as many words as make the last round of tiles a full one, if those are at least five eighths of it: 8 tokens of
+  // 4,096 columns into 100,260 76 us -> 70, into 40,000 28.3 -> 26.0, 32 of 8,192 into 50,000 75.7 -> 71.4; with half a tile 8 of 4,096 into
+  // 32,768 take 22.2, with all of it 21.3.
+  if (kSize == kFew) {
+    const int64_t places = ((int64_t)a.tiles + kSizes[kSize].at_once - 1) / kSizes[kSize].at_once * kSizes[kSize].at_once;
+    const int words = (int)((a.vocab + places - 1) / places + 3) / 4 * 4;
+    a.words = words * 8 >= kSizes[kSize].words * 5 ? words : kSizes[kSize].words;
+    a.tiles = blocks(a.vocab, a.words);
+  }
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(std::min(a.tiles, (unsigned)kSizes[kSize].at_once)), dim3(64 * kWm * kWv), 0, stream, a, out);
   };
@@ -57,7 +70,8 @@ template <typename T>
 void launch_size(Size size, const ProjectArgs& a, bool direct, T* out, hipStream_t stream) {
   if (size == kLarge) launch_tiles<T, kLarge, 4, 2, 2, 4, 2>(a, direct, out, stream);
   else if (size == kMiddle) launch_tiles<T, kMiddle, 2, 1, 2, 4, 2>(a, direct, out, stream);
-  else launch_tiles<T, kSmall, 1, 1, 2, 2, 4>(a, direct, out, stream);
+  else if (size == kSmall) launch_tiles<T, kSmall, 1, 1, 2, 2, 4>(a, direct, out, stream);
+  else launch_tiles<T, kFew, 1, 1, 1, 4, 3>(a, direct, out, stream);
 }
 
 template <typename T>

@@ -7,7 +7,7 @@
 // Measured on one MI355X, whose matrix units reach 3.5e15 operations/s on random bytes (they, too, lower the clock):
 //   8,191 tokens x 2,048 into 100,260 bfloat16   1,620 to 1,680 us, 2.0e15/s; 8,192 x 4,096 into 32,768 940 to 980 us, 2.3e15/s
 //   (torch's product with 32-bit sums written: 2,008 and 1,017 us)
-//   8 tokens x 4,096 into 100,260                 75 to 79 us, 5.2 to 5.5 TB/s: the reading of the weights
+//   8 tokens x 4,096 into 100,260                 70 us, 5.9 TB/s: the reading of the weights; 32 x 8,192 into 50,000 71 us, 5.7 TB/s
 // What the first of these spent at 1,700, by leaving parts out: products and readings of shared memory alone 1,130 us, with the stages' transfers
 // (13 GB through the second-level caches, 960 us alone) 1,380, with the conversion of the logits 1,500, the rest their stores; rows of
 // 100,260 begin at multiples of 8 bytes, and of 100,352 the stores take 120 less.  Stages of 64 bytes, four of them instead of two of 128: 1,800
@@ -31,6 +31,7 @@ struct ProjectArgs {
   int64_t n, vocab, q_stride, weight_stride, out_stride;
   int dim;
   unsigned token_tiles, tiles;                              // tiles: of the whole product
+  int words;                                                // of a tile for few tokens, at most its size
 };
 
 // Which tile a workgroup has.  Workgroups go round the eight dies; each die takes a stretch of the tiles of its own, in which up to
@@ -128,23 +129,26 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wave_token = wave / kWv * (32 * kMt), wave_word = wave % kWv * (32 * kVt);
   const int steps = (a.dim + kStep - 1) / kStep, ragged = a.dim % kStep ? steps - 1 : -1;
+  const int words = kTokens == 32 ? a.words : kWords;        // (few tokens: as many as share the work evenly)
   const unsigned mine = (a.tiles - blockIdx.x + gridDim.x - 1) / gridDim.x;
   // Workgroups begin at different columns, by thirty-seconds of a row, and go round: all at the same columns of rows of 4,096 bytes would
-  // ask the same parts of memory at once.  8 tokens x 4,096 into 100,260: 84 us -> 76; 32 x 8,192 into 50,000: 94 -> 84; 4,096 x 4,096 into
-  // 65,536: 993 -> 960; 8,191 x 2,048 into 100,260: 1,680 -> 1,630.  (Small tiles with the large ones' places 76, 87; large ones with the
-  // small ones' 980, 1,650.)
+  // ask the same parts of memory at once.  Tiles of 64 x 64 for 8 tokens x 4,096 into 100,260: 84 us -> 76; 32 x 8,192 into 50,000: 94 -> 84;
+  // of 256 x 256 for 4,096 x 4,096 into 65,536: 993 -> 960; 8,191 x 2,048 into 100,260: 1,680 -> 1,630.  (Small tiles with the large ones' places
+  // 76, 87; large ones with the small ones' 980, 1,650.)
   const unsigned die = blockIdx.x % kXcds, begin = kMt * kVt >= 8 ? die * 4 + blockIdx.x / kXcds % 4 : die % 4 * 8;
   const int first_step = (int)(begin * (unsigned)steps / 32);
 
   // Loading.  The 16 bytes c of row r lie at place c ^ turn(r): shared memory serves sixteen lanes at a time from 64 banks, and so sixteen
   // rows of the same columns lie in 256 bytes once.
-  // A wave's loads are of tokens or of weights alone.
+  // A load is of tokens or of weights alone, and, where the numbers of rows allow it, all of a wave's are.
   constexpr int kOwn = kRows / kWaves;
-  static_assert(kTokens % kOwn == 0);
-  const bool of_tokens = wave * kOwn < kTokens;
-  const int in_load = lane / kChunks, own_row = wave * kOwn - (of_tokens ? 0 : kTokens) + in_load;
+  constexpr bool kMixed = kTokens % kOwn != 0;
+  static_assert(kTokens % kAtOnce == 0);
+  const auto of_tokens = [&](int i) { return wave * kOwn + (kMixed ? i * kAtOnce : 0) < kTokens; };
+  const int in_load = lane / kChunks;
   const auto place = [&](int i) { return ((lane % kChunks) ^ turn<kStep>(wave * kOwn + i * kAtOnce + in_load)) * 16; };
-  const int8_t* from = nullptr;                              // the tile's first row
+  const int8_t* from[kMixed ? 2 : 1];                        // the tile's first row, of tokens and of weights or of this wave's
+  const auto first_row = [&](int i) { return kMixed && !of_tokens(i) ? from[kMixed] : from[0]; };
   uint32_t offset[kLoads];                                   // of each load's row and this lane's place in it, from there
   Bytes16 held[kDirect ? 1 : kLoads];
   unsigned fetch_tile = 0;
@@ -152,13 +156,15 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
   const auto begin_fetch = [&] {
     if (fetch_step != first_step || fetch_tile >= mine) return;
     const Tile tile = tile_of(blockIdx.x + fetch_tile * gridDim.x, a.token_tiles, a.tiles);
-    const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * kWords;
-    from = of_tokens ? a.q + token * a.q_stride : a.weight + word * a.weight_stride;
-    const int64_t last = (of_tokens ? a.n - token : a.vocab - word) - 1;
-    const uint32_t stride = (uint32_t)(of_tokens ? a.q_stride : a.weight_stride);
+    const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * words;
+    from[0] = kMixed || of_tokens(0) ? a.q + token * a.q_stride : a.weight + word * a.weight_stride;
+    if (kMixed) from[kMixed] = a.weight + word * a.weight_stride;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)                         // (rows behind the last: the last once more, nobody stores their logits)
-      offset[i] = (uint32_t)min((int64_t)(own_row + i * kAtOnce), last) * stride + (uint32_t)place(i);
+    for (int i = 0; i < kLoads; ++i) {                       // (rows behind the last: the last once more, nobody stores their logits)
+      const int64_t last = (of_tokens(i) ? a.n - token : min((int64_t)words, a.vocab - word)) - 1;
+      const uint32_t stride = (uint32_t)(of_tokens(i) ? a.q_stride : a.weight_stride);
+      offset[i] = (uint32_t)min((int64_t)(wave * kOwn - (of_tokens(i) ? 0 : kTokens) + in_load + i * kAtOnce), last) * stride + (uint32_t)place(i);
+    }
     for (int i = wave * 64; i < kRows; i += kWaves * 64) {
       const int row = i + lane;
       const float* p = row < kTokens ? a.scales + min(token + row, a.n - 1) : a.weight_scales + min(word + row - kTokens, a.vocab - 1);
@@ -167,19 +173,18 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
   };
   const auto fetch = [&] {
     int8_t* to = stages + fetch_stage * kStage + wave * kLoads * 1024;
-    const int8_t* here = from + fetch_step * kStep;
     if (fetch_step != ragged) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        if constexpr (kDirect) transfer<16>(here + offset[i], to + i * 1024);
-        else held[i] = load_bytes(here + offset[i]);
+        if constexpr (kDirect) transfer<16>(first_row(i) + fetch_step * kStep + offset[i], to + i * 1024);
+        else held[i] = load_bytes(first_row(i) + fetch_step * kStep + offset[i]);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int at = fetch_step * kStep + place(i);
-        if constexpr (kDirect) transfer<16>(from + (offset[i] - (uint32_t)place(i) + (uint32_t)min(at, a.dim - 16)), to + i * 1024);
-        else held[i] = load_end(from + (offset[i] - (uint32_t)place(i)), at, a.dim);
+        if constexpr (kDirect) transfer<16>(first_row(i) + (offset[i] - (uint32_t)place(i) + (uint32_t)min(at, a.dim - 16)), to + i * 1024);
+        else held[i] = load_end(first_row(i) + (offset[i] - (uint32_t)place(i)), at, a.dim);
         if constexpr (!kDirect) __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -230,7 +235,7 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
   int stage = 0, stored = 0;                                 // stored: of how many steps to come the stages are older than a whole tile's stores
   for (unsigned t = 0; t < mine; ++t) {
     const Tile tile = tile_of(blockIdx.x + t * gridDim.x, a.token_tiles, a.tiles);
-    const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * kWords;
+    const int64_t token = (int64_t)tile.token * kTokens, word = (int64_t)tile.word * words;
 #pragma unroll 1
     for (int count = 0, step = first_step; count < steps; ++count, step = step + 1 == steps ? 0 : step + 1) {
       const int next = stage + 1 == kStages ? 0 : stage + 1;
@@ -281,7 +286,7 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
     // memory of its own, 64 bytes of some tokens at a time; its accesses are in order by themselves.
     const float* scales = tile_scales + t % kScaleSets * kScales;
     int8_t* corner = corners + wave * kOutTokens * kOutRow;
-    const bool whole = token + kTokens <= a.n && word + kWords <= a.vocab;
+    const bool whole = token + kTokens <= a.n && words == kWords && word + kWords <= a.vocab;
     constexpr int kWidth = Vec<T>::kWidth, kEights = 8 / (int)sizeof(T);           // groups of eight words in 64 bytes
 #pragma unroll
     for (int m = 0; m < kMt; ++m) {
@@ -321,7 +326,7 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
             } else if (to < a.n) {
               float z[kWidth];
               y.get(z);
-              const int64_t left = a.vocab - word - column;
+              const int64_t left = min((int64_t)words, a.vocab - word) - column;
               if (left >= kWidth) y.store(p);
               else
                 for (int j = 0; j < kWidth; ++j)

@@ -78,6 +78,29 @@ def test_many_tiles_of_a_workgroup(n, dim):
             assert torch.equal(bpe.project_8bit(q, scales, weight, weight_scales, dtype), want)
 
 
+@pytest.mark.parametrize("dim", [7, 16, 100, 387, 1029, 2048])
+@pytest.mark.parametrize("n", [1, 20, 31, 32])
+def test_few_tokens_and_large_vocabularies(n, dim):
+    """About the vocabularies from which few tokens have tiles of their own, and with a second tile for some workgroups."""
+    import paper_2507_11941_amd as bpe
+
+    for vocab, dtype, spread in ((16384, torch.bfloat16, 0), (16385, torch.float32, 4), (16512, torch.float16, 0), (30001, torch.bfloat16, 3),
+                                 (65537, torch.bfloat16, 0)):
+        print(n, dim, vocab, flush=True)
+        q, weight = bytes_of(n, dim, 1, spread), bytes_of(vocab, dim, 2, spread)
+        scales, weight_scales = scales_of(n, 3), scales_of(vocab, 4)
+        # (whole numbers below 2^53; what the kernel rounds: the sum, its products with either scale, the result)
+        want = ((q.double() @ weight.double().t()).float() * scales[:, None] * weight_scales).to(dtype)
+        room = torch.full((n + 2, vocab + 5), 3.0, dtype=dtype, device=dev())
+        out = room[1:-1, 2:vocab + 2]
+        for _ in range(3):
+            assert torch.equal(bpe.project_8bit(q, scales, weight, weight_scales, dtype), want)
+            bpe.project_8bit(q, scales, weight, weight_scales, out=out)
+            assert torch.equal(out, want)
+        out.fill_(3.0)
+        assert bool((room == 3.0).all())
+
+
 @pytest.mark.parametrize("n", [9, 60, 130])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_nothing_else_is_written(n, dtype):
