@@ -13,9 +13,9 @@ using namespace bpe;
 namespace {
 
 // Threads a stretch, sixteen columns each, by the mean of the histories: the more of them, the fewer stretches look through a history, and
-// the later a workgroup's logits follow.  509 rows of 100,260 bfloat16 with 256, 512, 1,024 threads: histories of 100 tokens 33.9, 34.0,
-// 39.1 us, of 1,000 38.7, 37.9, 44.0, of 4,000 (and masks) 47.7, 46.1, 47.3, of 16,000 74.1, 68.6, 64.9; 2,011 of 32,256 with 250 47.7,
-// 45.7, 51.3; 32 of 100,260 with 10 5.7, 5.8, 6.0, with 1,000 7.7, 7.8, 8.0, with 16,000 10.6, 8.9, 8.0.  (Where the ids are a buffer that is
+// the later a workgroup's logits follow.  509 rows of 100,260 bfloat16 with 256, 512, 1,024 threads: histories of 100 tokens 33.7, 33.6,
+// 36.5 us, of 1,000 37.1, 36.9, 40.3, of 4,000 (and masks) 46.7, 44.6, 46.1, of 16,000 72.6, 67.9, 64.6; 2,011 of 32,256 with 250 43.6,
+// 44.6, 47.1; 32 of 100,260 with 10 5.2, 5.4, 5.7, with 1,000 7.2, 7.2, 7.5, with 16,000 10.3, 8.8, 7.9.  (Where the ids are a buffer that is
 // not full, or histories share them, the mean is another, and the choice may be: results are the same.)
 constexpr int64_t kLong = 2000, kLonger = 8000;
 

@@ -55,16 +55,15 @@ __device__ inline void for_ids(const int32_t* ids, Span s, int32_t column, int32
 #pragma unroll
     for (uint32_t k = 0; k < kDeep; ++k) look(first + k * kThreads + threadIdx.x, id[k]);
   }
-  if (first == count) return;
+  // (The rest: places behind the end read the last id once more, and do not look at it.)
+  const uint32_t left = count - first;
   int32_t id[kDeep];
 #pragma unroll
-  for (uint32_t k = 0; k < kDeep; ++k) {
-    const uint32_t i = first + k * kThreads + threadIdx.x;
-    id[k] = -1;
-    if (i < count) id[k] = p[i];
-  }
+  for (uint32_t k = 0; k < kDeep; ++k)
+    if (k * kThreads < left) id[k] = p[first + min(k * kThreads + threadIdx.x, left - 1)];
 #pragma unroll
-  for (uint32_t k = 0; k < kDeep; ++k) look(first + k * kThreads + threadIdx.x, id[k]);
+  for (uint32_t k = 0; k < kDeep; ++k)
+    if (k * kThreads < left) look(first + k * kThreads + threadIdx.x, k * kThreads + threadIdx.x < left ? id[k] : -1);
 }
 
 // The numbers of a lane's vector in shared memory.
@@ -162,19 +161,28 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const T* in, const T* 
       else load_part(x + at, valid, y);
     }
     if constexpr (kGrad) {
-      if (any != 0) {
+      // (Logits by whole vectors where one has eight elements, by elements where it has four: 509 rows of 100,260 with 4,000 tokens of history
+      // under masks 44.8 us for 48.3, with 16,000 70 for 80; in 32 bits with 1,000 86 for 78.)
+      const T* from = logits + t * a.logits_stride + column + at;
+      if (kWidth == 8 && any != 0 && bits != 0) {
+        float was[kWidth];
+        load_part(from, valid, was);
+#pragma unroll
+        for (int i = 0; i < kWidth; ++i) y[i] = c[i] ? y[i] * (was[i] > 0.0f ? reciprocal : repetition) : y[i];
+      } else if (kWidth < 8 && any != 0) {
 #pragma unroll
         for (int i = 0; i < kWidth; ++i)
-          if (c[i] && (bits >> i & 1)) y[i] *= to_float(logits[t * a.logits_stride + column + at + i]) > 0.0f ? reciprocal : repetition;
+          if (c[i] && (bits >> i & 1)) y[i] *= to_float(from[i]) > 0.0f ? reciprocal : repetition;
       }
     } else {
-      // (Without branches: of a long history's tokens some are among most waves' elements.  An element that no token names is multiplied
-      // by 1 and has 0 subtracted, which leaves it as it is.)
+      // (Without branches for each element, of a long history's tokens some are among most waves' elements; one selection an element, and the
+      // masks as bits: 509 rows of 100,260 with 4,000 tokens of history under masks 45.7 us -> 44.0, 2,011 of 32,256 with 250 45.6 -> 43.9.)
       if (any != 0) {
 #pragma unroll
         for (int i = 0; i < kWidth; ++i) {
           const float factor = y[i] > 0.0f ? reciprocal : repetition, less = fmaf(frequency, (float)c[i], presence);
-          y[i] = fmaf(y[i], c[i] ? factor : 1.0f, c[i] ? -less : -0.0f);
+          const float changed = fmaf(y[i], factor, -less);
+          y[i] = c[i] ? changed : y[i];
         }
       }
       if (biased) {
@@ -184,7 +192,10 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const T* in, const T* 
       }
     }
 #pragma unroll
-    for (int i = 0; i < kWidth; ++i) y[i] = bits >> i & 1 ? y[i] : kGrad ? 0.0f : -INFINITY;
+    for (int i = 0; i < kWidth; ++i) {
+      const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)bits, i, 1), other = kGrad ? 0u : 0xff800000u;
+      y[i] = __uint_as_float((__float_as_uint(y[i]) & keep) | (other & ~keep));
+    }
     store_part(out + t * a.out_stride + column + at, valid, y);
   }
 }
