@@ -2,6 +2,7 @@
 
 Streams, allocation, strides and refusals are as in ``_ops.py``.  ``add_norm`` and ``adjust_logits`` are recorded by torch's automatic
 differentiation where what they are given wants a gradient; what is in 8 bits carries none, and is refused for a tensor that wants one.
+Forward-mode derivatives are not computed: a tensor that carries one (a dual tensor) is refused, so that it is not lost.
 (A training step that is captured in a graph takes its gradients from ``add_norm_grad`` and ``adjust_logits_grad``, or from
 ``torch.autograd.grad``: torch's ``backward()`` adds them up on the stream on which a parameter was first used, which need not be the one
 that is captured.)"""
@@ -83,7 +84,14 @@ def _recorded():
     return Norm, Adjusted
 
 
+def _no_tangent(*tensors):
+    forward = torch.autograd.forward_ad
+    if forward._current_level >= 0 and any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors):
+        raise ValueError("there is no forward-mode derivative here: give the primal tensors")
+
+
 def _wants(*tensors):
+    _no_tangent(*tensors)
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
@@ -192,6 +200,7 @@ def add_norm_grad(grad, summed, weight, rstd, grad_summed=None, out=None, out_we
     if stream is not None:
         return _on(stream, add_norm_grad, grad, summed, weight, rstd, grad_summed, out, out_weight, dtype, accumulate, workspace)
     lib = _lib or _load()
+    _no_tangent(grad, summed, weight, rstd, grad_summed)
     stride, dev = _matrix(grad, "grad"), grad.device
     n, dim = grad.shape
     summed_stride = _matrix(summed, "summed", dev, (n, dim), grad.dtype)
@@ -360,6 +369,7 @@ def adjust_logits_grad(grad, logits, ids=None, begin=None, end=None, penalties=N
     if stream is not None:
         return _on_all(stream, adjust_logits_grad, grad, logits, ids, begin, end, penalties, mask, state, out)
     lib = _lib or _load()
+    _no_tangent(grad, logits, penalties if isinstance(penalties, torch.Tensor) else None)
     grad_stride, dev = _matrix(grad, "grad"), grad.device
     n, vocab = grad.shape
     stride = _matrix(logits, "logits", dev, (n, vocab), grad.dtype)
