@@ -24,7 +24,8 @@ extern "C" {
  *                              x or the residual, but not summed (same pointer and stride); else nothing that is written overlaps
  *                              anything.
  *   weight  [dim] of weight_dtype: BPE_F32 or `dtype`;  rstd float[n], or NULL.
- *   eps     >= 0.  A row of zeros with eps = 0 gives NaN, as do infinities and NaN in a row. */
+ *   eps     >= 0.  A row of zeros with eps = 0 gives NaN, as does a row with a NaN; one with infinities gives NaN where they are, else 0.
+ *           Of rows whose root mean square is below 2^-128 (with eps = 0) rstd is infinite; out is the formula's all the same. */
 int bpe_add_norm(const void* x, int dtype, int64_t n, int64_t dim, int64_t stride, const void* residual, int64_t residual_stride,
                  const void* weight, int weight_dtype, float eps, void* summed, int64_t summed_stride, float* rstd, void* out,
                  int64_t out_stride, void* stream);
@@ -41,7 +42,8 @@ int bpe_add_norm_8bit(const void* x, int dtype, int64_t n, int64_t dim, int64_t 
 /* The gradients of a norm.  With u_j = grad[t][j] weight[j], h_j = s_j rstd[t] and m = mean over j of u_j h_j,
  *   grad_x[t][j] = rstd[t] (u_j - h_j m) + grad_summed[t][j],   which is the residual's gradient as well;
  *   grad_weight[j] = sum over t of grad[t][j] h_j, with `accumulate` != 0 added to what it holds.
- *   grad, summed (x where there was no residual), grad_x  [n][dim] of `dtype`;  rstd as bpe_add_norm wrote it.
+ *   grad, summed (x where there was no residual), grad_x  [n][dim] of `dtype`;  rstd as bpe_add_norm wrote it (of a row whose rstd is
+ *   infinite the gradients are no numbers).
  *   grad_summed  of the same, or NULL: zeros.  grad_x may be grad or grad_summed (same pointer and stride), else overlaps nothing.
  *   grad_weight  [dim] of grad_weight_dtype: BPE_F32 or weight_dtype; or NULL: not wanted. */
 int bpe_add_norm_grad(const void* grad, int dtype, int64_t n, int64_t dim, int64_t grad_stride, const void* summed,
