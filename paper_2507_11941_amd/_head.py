@@ -337,10 +337,15 @@ def adjust_logits(logits, ids=None, begin=None, end=None, penalties=None, bias=N
     ``mask``: int32 [states, ceil(vocab / 32)], where a token's bit is 0 its logit becomes -inf; ``state`` (int32 [n]) is each row's mask
     (outside [0, states): none), and may be left out with one mask for all rows or one for each.  ``out`` may be ``logits`` itself: only
     what changes is written then.  Part of torch's backward pass where logits want a gradient (``out`` cannot be given then)."""
+    if bias is not None:
+        bias = tuple(bias)
+        if len(bias) != 4:
+            raise ValueError("bias must be ids, values, begin and end")
     if stream is not None:
         return _on_all(stream, adjust_logits, logits, ids, begin, end, penalties, bias, mask, state, out)
     lib = _lib or _load()
-    _no_gradient("what logits are adjusted by", penalties if isinstance(penalties, torch.Tensor) else None, bias and bias[1])
+    _no_gradient("what logits are adjusted by", penalties if isinstance(penalties, torch.Tensor) else None,
+                 None if bias is None else bias[1])
     if _wants(logits):
         if out is not None:
             raise ValueError("out cannot be recorded by automatic differentiation: give logits.detach(), or call under torch.no_grad()")
