@@ -70,8 +70,10 @@ def _recorded():
         @staticmethod
         def forward(ctx, logits, ids, begin, end, penalties, bias, mask, state):
             rows = penalties if isinstance(penalties, torch.Tensor) else None
+            if rows is None and penalties is not None:
+                penalties = tuple(penalties)                 # (a list may be another one by the backward pass)
             ctx.save_for_backward(logits, ids, begin, end, rows, mask, state)
-            ctx.penalties = penalties
+            ctx.penalties = None if rows is not None else penalties
             return adjust_logits(logits, ids, begin, end, penalties, bias, mask, state)
 
         @staticmethod
