@@ -45,7 +45,7 @@ int bpe_add_norm_8bit(const void* x, int dtype, int64_t n, int64_t dim, int64_t 
  *   grad, summed (x where there was no residual), grad_x  [n][dim] of `dtype`;  rstd as bpe_add_norm wrote it (of a row whose rstd is
  *   infinite the gradients are no numbers).
  *   grad_summed  of the same, or NULL: zeros.  grad_x may be grad or grad_summed (same pointer and stride), else overlaps nothing.
- *   grad_weight  [dim] of grad_weight_dtype: BPE_F32 or weight_dtype; or NULL: not wanted. */
+ *   grad_weight  [dim] of grad_weight_dtype: BPE_F32 or weight_dtype; or NULL: not wanted, and no workspace needed. */
 int bpe_add_norm_grad(const void* grad, int dtype, int64_t n, int64_t dim, int64_t grad_stride, const void* summed,
                       int64_t summed_stride, const void* weight, int weight_dtype, const float* rstd, const void* grad_summed,
                       int64_t grad_summed_stride, void* grad_x, int64_t grad_x_stride, void* grad_weight, int grad_weight_dtype,

@@ -63,7 +63,7 @@ def _recorded():
             if grad is None:
                 return grad_summed, None, grad_summed, None
             grad_summed = None if grad_summed is None else grad_summed.contiguous()
-            grad_x, grad_weight = add_norm_grad(grad.contiguous(), summed, weight, rstd, grad_summed)
+            grad_x, grad_weight = add_norm_grad(grad.contiguous(), summed, weight, rstd, grad_summed, weights=ctx.needs_input_grad[1])
             return grad_x, grad_weight, grad_x if ctx.needs_input_grad[2] else None, None
 
     class Adjusted(torch.autograd.Function):
@@ -194,13 +194,14 @@ def add_norm_8bit(x, weight, residual=None, eps: float = 1e-6, summed=None, stre
 
 
 def add_norm_grad(grad, summed, weight, rstd, grad_summed=None, out=None, out_weight=None, dtype=None, accumulate: bool = False,
-                  workspace=None, stream=None):
+                  workspace=None, stream=None, *, weights: bool = True):
     """(gradient of x, which is the residual's as well, gradient of the weights) from that of the norm and that of the sum, if it was
     used besides, with the sum and ``rstd`` that ``add_norm`` returned.  The weights' gradient has ``out_weight``'s type or ``dtype``:
-    float32 or weight's (the default); with ``accumulate`` it is added to what ``out_weight`` holds.  ``out`` may be ``grad`` or
-    ``grad_summed`` itself."""
+    float32 or weight's (the default); with ``accumulate`` it is added to what ``out_weight`` holds; without ``weights`` it is not
+    computed (None).  ``out`` may be ``grad`` or ``grad_summed`` itself."""
     if stream is not None:
-        return _on(stream, add_norm_grad, grad, summed, weight, rstd, grad_summed, out, out_weight, dtype, accumulate, workspace)
+        return _on(stream, lambda *args: add_norm_grad(*args, weights=weights), grad, summed, weight, rstd, grad_summed, out, out_weight, dtype,
+                   accumulate, workspace)
     lib = _lib or _load()
     _no_tangent(grad, summed, weight, rstd, grad_summed)
     stride, dev = _matrix(grad, "grad"), grad.device
@@ -210,29 +211,34 @@ def add_norm_grad(grad, summed, weight, rstd, grad_summed=None, out=None, out_we
     rstd_ptr = _vector(rstd, "rstd", dev, torch.float32, n)
     more_stride = 0 if grad_summed is None else _matrix(grad_summed, "grad_summed", dev, (n, dim), grad.dtype)
     out_stride = dim if out is None else _matrix(out, "out", dev, (n, dim), grad.dtype)
-    if out_weight is None:
-        if accumulate:
-            raise ValueError("accumulate needs out_weight")
-        kind = dtype or weight.dtype
+    if not weights:
+        if accumulate or any(t is not None for t in (out_weight, dtype, workspace)):
+            raise ValueError("out_weight, dtype, accumulate and workspace are for the weights' gradient")
+        kind = torch.float32
     else:
-        kind = out_weight.dtype
-        if dtype is not None and kind != dtype:
-            raise ValueError(f"out_weight is {kind}, not {dtype}")
-        _vector(out_weight, "out_weight", dev, kind, dim)
-    if kind not in (torch.float32, weight.dtype):
-        raise ValueError(f"the weights' gradient must be float32 or {weight.dtype}")
-    workspace = _workspace(workspace, lib.bpe_add_norm_grad_workspace_bytes(n, dim), dev, "add_norm_grad")
+        if out_weight is None:
+            if accumulate:
+                raise ValueError("accumulate needs out_weight")
+            kind = dtype or weight.dtype
+        else:
+            kind = out_weight.dtype
+            if dtype is not None and kind != dtype:
+                raise ValueError(f"out_weight is {kind}, not {dtype}")
+            _vector(out_weight, "out_weight", dev, kind, dim)
+        if kind not in (torch.float32, weight.dtype):
+            raise ValueError(f"the weights' gradient must be float32 or {weight.dtype}")
+        workspace = _workspace(workspace, lib.bpe_add_norm_grad_workspace_bytes(n, dim), dev, "add_norm_grad")
     if out is None:
         out = grad.new_empty((n, dim))
     else:
         _written((out,))
-    if out_weight is None:
-        out_weight = torch.empty(dim, dtype=kind, device=dev)
-    else:
+    if out_weight is not None:
         _written((out_weight,))
+    elif weights:
+        out_weight = torch.empty(dim, dtype=kind, device=dev)
     _enqueue(lib.bpe_add_norm_grad, dev, grad.data_ptr(), _TYPES[grad.dtype], n, dim, stride, summed.data_ptr(), summed_stride, weight_ptr,
-             weight_type, rstd_ptr, _pointer(grad_summed), more_stride, out.data_ptr(), out_stride, out_weight.data_ptr(), _TYPES[kind],
-             1 if accumulate else 0, workspace.data_ptr(), workspace.numel())
+             weight_type, rstd_ptr, _pointer(grad_summed), more_stride, out.data_ptr(), out_stride, _pointer(out_weight), _TYPES[kind],
+             1 if accumulate else 0, _pointer(workspace), 0 if workspace is None else workspace.numel())
     return out, out_weight
 
 

@@ -116,7 +116,8 @@ def _on(stream, function, *args):
         if isinstance(t, torch.Tensor):
             t.record_stream(stream)
     for t in results if isinstance(results, tuple) else (results,):
-        t.record_stream(caller)
+        if t is not None:
+            t.record_stream(caller)
     return results
 
 
