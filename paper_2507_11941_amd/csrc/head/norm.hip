@@ -73,12 +73,16 @@ bool with_grad_variant(int64_t dim, F&& f) {
   return true;
 }
 
+// Whether what is written at p begins where q does without lying as q does: its rows would lie over other rows of q.
+bool crosses(const void* p, int64_t stride, const void* q, int64_t q_stride, int64_t n) { return p == q && n > 1 && stride != q_stride; }
+
 // Arguments that the two forms of the norm share.
 bool is_norm(const void* x, int dtype, int64_t n, int64_t dim, int64_t stride, const void* residual, int64_t residual_stride,
              const void* weight, int weight_dtype, float eps, const void* summed, int64_t summed_stride) {
   return is_count(n) && is_matrix(x, dtype, n, dim, stride) && (weight_dtype == BPE_F32 || weight_dtype == dtype) &&
          fits(weight, dim, size_of(weight_dtype)) && eps >= 0.0f && std::isfinite(eps) && !residual == !summed &&
-         (!residual || (is_matrix(residual, dtype, n, dim, residual_stride) && is_matrix(summed, dtype, n, dim, summed_stride)));
+         (!residual || (is_matrix(residual, dtype, n, dim, residual_stride) && is_matrix(summed, dtype, n, dim, summed_stride) &&
+                        !crosses(summed, summed_stride, x, stride, n) && !crosses(summed, summed_stride, residual, residual_stride, n)));
 }
 
 template <typename T, typename W>
@@ -109,7 +113,8 @@ int bpe_add_norm(const void* x, int dtype, int64_t n, int64_t dim, int64_t strid
                  const void* weight, int weight_dtype, float eps, void* summed, int64_t summed_stride, float* rstd, void* out,
                  int64_t out_stride, void* stream) {
   if (!is_norm(x, dtype, n, dim, stride, residual, residual_stride, weight, weight_dtype, eps, summed, summed_stride) ||
-      !aligned(rstd, 4) || !is_matrix(out, dtype, n, dim, out_stride) || (summed && out == summed && n > 0))
+      !aligned(rstd, 4) || !is_matrix(out, dtype, n, dim, out_stride) || (summed && out == summed && n > 0) ||
+      crosses(out, out_stride, x, stride, n) || (residual && crosses(out, out_stride, residual, residual_stride, n)))
     return BPE_EINVAL;
   with_types(dtype, weight_dtype, [&](auto type, auto weight_type) {
     using T = decltype(type);
@@ -169,7 +174,8 @@ int bpe_add_norm_grad(const void* grad, int dtype, int64_t n, int64_t dim, int64
                       int accumulate, void* workspace, size_t workspace_bytes, void* stream_ptr) {
   if (!is_count(n) || !is_matrix(grad, dtype, n, dim, grad_stride) || !is_matrix(summed, dtype, n, dim, summed_stride) ||
       (weight_dtype != BPE_F32 && weight_dtype != dtype) || !fits(weight, dim, size_of(weight_dtype)) || !fits(rstd, n, 4) ||
-      (grad_summed && !is_matrix(grad_summed, dtype, n, dim, grad_summed_stride)) || !is_matrix(grad_x, dtype, n, dim, grad_x_stride))
+      (grad_summed && !is_matrix(grad_summed, dtype, n, dim, grad_summed_stride)) || !is_matrix(grad_x, dtype, n, dim, grad_x_stride) ||
+      crosses(grad_x, grad_x_stride, grad, grad_stride, n) || (grad_summed && crosses(grad_x, grad_x_stride, grad_summed, grad_summed_stride, n)))
     return BPE_EINVAL;
   if (grad_weight && ((grad_weight_dtype != BPE_F32 && grad_weight_dtype != weight_dtype) || !aligned(grad_weight, size_of(grad_weight_dtype)) ||
                       !is_workspace(workspace, workspace_bytes, bpe_add_norm_grad_workspace_bytes(n, dim))))
