@@ -76,7 +76,7 @@ int bpe_project_8bit(const int8_t* q, int64_t n, int64_t dim, int64_t q_stride, 
  *   c > 0:  x = x > 0 ? x / repetition : x * repetition;  x = x - (presence + frequency * c)      (divided by the rounded reciprocal)
  *   v is bias_ids[i] for an i in bias_begin[t] .. bias_end[t] - 1:  x = x + bias_values[i]; of several such i the last one counts
  *   bit v % 32 of mask[state[t]][v / 32] is 0:  x = -infinity, whatever it was.
- *   penalties   float[n][3]: repetition (> 0), presence and frequency of each row; or NULL: those given for all rows.
+ *   penalties   float[n][3]: repetition (2^-126 to 2^126), presence and frequency of each row; or NULL: those given for all rows.
  *   ids         int32[n_ids]; begin, end int64[n].  begin and end may be NULL: no history.  (Of a history or a list of biases the first
  *               0xfffffff0 are looked at.)
  *   bias_ids, bias_values   int32 and float [n_biases]; bias_begin, bias_end int64[n], bounds as above; both may be NULL: no biases.

@@ -73,7 +73,8 @@ AdjustArgs adjust_args(int64_t vocab, int64_t stride, const int32_t* ids, int64_
   return a;
 }
 
-bool is_repetition(float r) { return r > 0.0f && std::isfinite(r); }
+// (Logits are multiplied by its reciprocal, which has to be an ordinary number too.)
+bool is_repetition(float r) { return r >= 0x1p-126f && r <= 0x1p126f; }
 
 }  // namespace
 
