@@ -62,8 +62,8 @@ void launch_tiles(ProjectArgs a, bool direct, T* out, hipStream_t stream) {
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(std::min(a.tiles, (unsigned)kSizes[kSize].at_once)), dim3(64 * kWm * kWv), 0, stream, a, out);
   };
-  if (direct) launch(project_kernel<T, kMt, kVt, kWm, kWv, kStages, 128, true>);
-  else launch(project_kernel<T, kMt, kVt, kWm, kWv, 2, 128, false>);
+  if (direct) launch(project_kernel<T, kMt, kVt, kWm, kWv, kStages, true>);
+  else launch(project_kernel<T, kMt, kVt, kWm, kWv, 2, false>);
 }
 
 template <typename T>

@@ -22,6 +22,7 @@ typedef int Bytes16 __attribute__((ext_vector_type(4)));
 typedef int Sums __attribute__((ext_vector_type(16)));
 
 constexpr int kXcds = 8;
+constexpr int kStep = 128;                                  // bytes of a row in a stage
 
 struct ProjectArgs {
   const int8_t* q;
@@ -71,8 +72,7 @@ __device__ inline void transfer(const void* from, void* to) {
 }
 
 // How far the chunks of 16 bytes of a row are turned.
-template <int kStep>
-__device__ inline int turn(int row) { return kStep == 128 ? row >> 1 & 7 : row >> 2 & 3; }
+__device__ inline int turn(int row) { return row >> 1 & 7; }
 
 // 16 bytes at any address.
 __device__ inline Bytes16 load_bytes(const int8_t* p) {
@@ -107,17 +107,17 @@ __device__ inline int keeps(int cleared, int word) {
   return bytes >= 4 ? 0 : bytes <= 0 ? -1 : -1 << (8 * bytes);
 }
 
-// kMt x kVt tiles of 32 x 32 a wave (tokens x vocabulary), kWm x kWv waves; kStages stages of kStep bytes of each row.  With kDirect rows
+// kMt x kVt tiles of 32 x 32 a wave (tokens x vocabulary), kWm x kWv waves; kStages stages.  With kDirect rows
 // begin at multiples of 4 bytes and have a multiple of 4, at least 16, and go from memory into shared memory by themselves; else through
 // registers.  A workgroup has tiles gridDim.x apart, and the stages go on from one to the next: while a tile's logits are written, the
 // next one's first stages are on their way.  (Behind the last tile stages are fetched once more, and not used: the loop has no branches.)
-template <typename T, int kMt, int kVt, int kWm, int kWv, int kStages, int kStep, bool kDirect>
+template <typename T, int kMt, int kVt, int kWm, int kWv, int kStages, bool kDirect>
 __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, T* out) {
   constexpr int kWaves = kWm * kWv, kTokens = 32 * kMt * kWm, kWords = 32 * kVt * kWv;
   constexpr int kRows = kTokens + kWords, kStage = kRows * kStep;
   constexpr int kChunks = kStep / 16, kAtOnce = 64 / kChunks, kLoads = kRows / kAtOnce / kWaves;      // chunks of a row; rows of a load
   constexpr int kParts = kStep / 32, kSets = kDirect ? 2 : 1;      // parts of a step: products of 32 bytes of each row
-  static_assert(kRows % (kAtOnce * kWaves) == 0 && (kStep == 64 || kStep == 128) && (kDirect || kStages == 2));
+  static_assert(kRows % (kAtOnce * kWaves) == 0 && (kDirect || kStages == 2));
   constexpr int kOutTokens = kMt * kVt >= 8 ? 32 : 16;       // whose logits are in a wave's corner at once: what there is room for
   constexpr int kOutRow = 64 + 16;                           // 64 bytes of a token's logits, and room between rows
   constexpr int kStores = kMt * kVt * (int)sizeof(T);        // of a tile, by each wave
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
   static_assert(kTokens % kAtOnce == 0);
   const auto of_tokens = [&](int i) { return wave * kOwn + (kMixed ? i * kAtOnce : 0) < kTokens; };
   const int in_load = lane / kChunks;
-  const auto place = [&](int i) { return ((lane % kChunks) ^ turn<kStep>(wave * kOwn + i * kAtOnce + in_load)) * 16; };
+  const auto place = [&](int i) { return ((lane % kChunks) ^ turn(wave * kOwn + i * kAtOnce + in_load)) * 16; };
   const int8_t* from[kMixed ? 2 : 1];                        // the tile's first row, of tokens and of weights or of this wave's
   const auto first_row = [&](int i) { return kMixed && !of_tokens(i) ? from[kMixed] : from[0]; };
   uint32_t offset[kLoads];                                   // of each load's row and this lane's place in it, from there
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(64 * kWm * kWv) project_kernel(ProjectArgs a, 
   const int row = lane & 31, half = lane >> 5;
   Bytes16 x[kSets][kMt], w[kSets][kVt];
   const auto read = [&](int stage, int part) {
-    const int8_t* here = stages + stage * kStage + row * kStep + ((2 * part + half) ^ turn<kStep>(row)) * 16;
+    const int8_t* here = stages + stage * kStage + row * kStep + ((2 * part + half) ^ turn(row)) * 16;
 #pragma unroll
     for (int v = 0; v < kVt; ++v) w[part % kSets][v] = *(const Bytes16*)(here + (kTokens + wave_word + v * 32) * kStep);
 #pragma unroll
