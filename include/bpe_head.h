@@ -57,7 +57,8 @@ size_t bpe_add_norm_grad_workspace_bytes(int64_t n, int64_t dim);
 int bpe_quantize_rows(const void* x, int dtype, int64_t n, int64_t dim, int64_t stride, int8_t* q, int64_t q_stride, float* scales,
                       void* stream);
 
-/* out[t][v] = scales[t] * weight_scales[v] * (sum over k of q[t][k] weight[v][k]); the sum is exact.
+/* out[t][v] = (sum over k of q[t][k] weight[v][k]) * scales[t] * weight_scales[v]; the sum is exact, then it and both products are rounded
+ * to 32 bits, in this order.
  *   q       int8 [n][dim], dim <= BPE_MAX_DIM_8BIT (the sum fits 32 bits);  scales float[n]
  *   weight  int8 [vocab][dim];  weight_scales float[vocab]
  *           both with a stride of at most BPE_MAX_STRIDE_8BIT
@@ -94,7 +95,7 @@ int bpe_adjust_logits(const void* logits, int dtype, int64_t n, int64_t vocab, i
 
 /* The gradient with respect to the logits, from that of what bpe_adjust_logits wrote: 0 where the mask's bit is 0, else grad[t][v],
  * and where v is in the history, grad[t][v] / repetition for logits[t][v] > 0 and grad[t][v] * repetition for others.
- *   logits  as they were before; only those of tokens in histories are read.
+ *   logits  as they were before; only those of tokens in histories matter, and with them up to 16 bytes of their row about each are read.
  *   out     [n][vocab] of `dtype`; may be grad (same pointer and stride), else overlaps nothing. */
 int bpe_adjust_logits_grad(const void* grad, int dtype, int64_t n, int64_t vocab, int64_t grad_stride, const void* logits,
                            int64_t stride, const int32_t* ids, int64_t n_ids, const int64_t* begin, const int64_t* end,
