@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 
 from . import _ops
-from ._ops import _enqueue, _matrix, _on, _pointer, _vector, _workspace
+from ._ops import _enqueue, _matrix, _no_tangent, _on, _pointer, _vector, _workspace
 
 _lib = torch = _Norm = _Adjusted = _TYPES = _written = None      # (the package can be imported without torch)
 
@@ -84,12 +84,6 @@ def _recorded():
             return adjust_logits_grad(grad.contiguous(), logits, ids, begin, end, penalties, mask, state), *[None] * 7
 
     return Norm, Adjusted
-
-
-def _no_tangent(*tensors):
-    forward = torch.autograd.forward_ad
-    if forward._current_level >= 0 and any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors):
-        raise ValueError("there is no forward-mode derivative here: give the primal tensors")
 
 
 def _wants(*tensors):

@@ -4,8 +4,9 @@ Every function enqueues on ``stream`` (default: torch's current stream of the te
 Outputs and workspaces that are not given are allocated, on that stream.  Matrices may have any stride between rows, but not
 between columns; vectors are contiguous.  What the kernels cannot take is refused (ValueError), never copied into shape.
 
-``embed_tokens`` is recorded by torch's automatic differentiation where its weight wants a gradient.  The functions on logits are not:
-their gradient is an output, which ``logits.backward(grad)`` hands on, and log-probabilities and losses carry none."""
+``embed_tokens`` is recorded by torch's automatic differentiation where its weight wants a gradient (not in forward mode, which it
+refuses).  The functions on logits are not: their gradient is an output, which ``logits.backward(grad)`` hands on, and
+log-probabilities and losses carry none."""
 from __future__ import annotations
 
 import ctypes
@@ -65,6 +66,13 @@ def _lookup():
             return embed_tokens_grad(grad.contiguous(), ids, ctx.vocab, ctx.scale, count), None, None, None
 
     return Lookup
+
+
+def _no_tangent(*tensors):
+    """Refuses tensors with a forward-mode derivative, which would be lost."""
+    forward = torch.autograd.forward_ad
+    if forward._current_level >= 0 and any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors):
+        raise ValueError("there is no forward-mode derivative here: give the primal tensors")
 
 
 def _matrix(t, what, dev=None, shape=None, dtype=None):
@@ -157,6 +165,7 @@ def embed_tokens(weight, ids, scale: float = 1.0, count=None, out=None, stream=N
     if stream is not None:
         return _on(stream, embed_tokens, weight, ids, scale, count, out)
     lib = _lib or _load()
+    _no_tangent(weight)
     if weight.requires_grad and torch.is_grad_enabled():
         if out is not None:
             raise ValueError("out cannot be recorded by automatic differentiation: give weight.detach(), or call under torch.no_grad()")
