@@ -52,3 +52,19 @@ def test_rows_of_zeros_and_odd_rows_are_as_they_were(dim):
         assert bool(torch.isnan(y[row, at])) and not y[row].nan_to_num().any() and float(rstd[row]) == 0.0
     y, _, _ = bpe.add_norm(x, torch.ones(dim, device=dev()))
     assert not y[0].any()
+
+
+@pytest.mark.parametrize("dim", [37, 1500, 20000])
+def test_in_place(dim):
+    """The norm in the place of x, and of the residual with the sum in that of x."""
+    import paper_2507_11941_amd as bpe
+
+    x = matrix(len(SIZES), dim, torch.float32, 5).cpu().double()
+    x = (x / x.abs().amax(1, keepdim=True) * torch.tensor(SIZES, dtype=torch.float64)[:, None]).float().to(dev())
+    weight, zeros = torch.linspace(0.5, 2, dim, device=dev()), torch.zeros_like(x)
+    want = bpe.add_norm(x, weight, None, 0.0)[0]
+    a = x.clone()
+    assert torch.equal(bpe.add_norm(a, weight, None, 0.0, out=a)[0], want)
+    a, b = x.clone(), zeros.clone()
+    got, total, _ = bpe.add_norm(a, weight, b, 0.0, out=b, summed=a)
+    assert torch.equal(got, want) and torch.equal(total, x)
