@@ -14,11 +14,11 @@ import ctypes
 from ._binding import _check, load_library
 
 _TYPES = {}                                      # torch dtype -> the library's number of it
-_lib = torch = _Lookup = _written = None         # (the package can be imported without torch)
+_lib = torch = _Lookup = _written = _forward = None      # (the package can be imported without torch)
 
 
 def _load():
-    global _lib, torch, _Lookup, _written
+    global _lib, torch, _Lookup, _written, _forward
     if _lib is None:
         import torch as module
 
@@ -43,7 +43,7 @@ def _load():
         lib.bpe_token_logprobs_workspace_bytes.restype = sz
         lib.bpe_loss_workspace_bytes.argtypes = [i64, i64, i32]
         lib.bpe_loss_workspace_bytes.restype = sz
-        _Lookup = _lookup()
+        _Lookup, _forward = _lookup(), torch.autograd.forward_ad
         _written = torch._C._increment_version   # (as in _binding.py; a call's own tensors only, given as a tuple)
         _TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
         _lib = lib
@@ -70,8 +70,7 @@ def _lookup():
 
 def _no_tangent(*tensors):
     """Refuses tensors with a forward-mode derivative, which would be lost."""
-    forward = torch.autograd.forward_ad
-    if forward._current_level >= 0 and any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors):
+    if _forward._current_level >= 0 and any(t is not None and _forward.unpack_dual(t).tangent is not None for t in tensors):
         raise ValueError("there is no forward-mode derivative here: give the primal tensors")
 
 
