@@ -530,7 +530,9 @@ __global__ void __launch_bounds__(kThreads) norm_grad_kernel(NormGradArgs<T, W> 
   if (tid < rest) to[edge_at] = edge_total;
 }
 
-// Rows that no workgroup's registers hold: the gradient of each row's elements, read twice and summed in 64 bits, ...
+// Rows that no workgroup's registers hold: the gradient of each row's elements, read twice and summed in 64 bits, ...  (An element a lane, and
+// with the weights' part three times through: 4,096 rows of 12,288 bfloat16 249 us, of 5,120 in 32 bits 111, where four matrices at 5 TB/s
+// would take 81 and 67.)
 template <typename T, typename W>
 __global__ void __launch_bounds__(1024) long_norm_grad_kernel(NormGradArgs<T, W> a, int64_t first) {
   constexpr int kThreads = 1024;

@@ -5,8 +5,9 @@
 // so that a lane holds four neighbours of a token's logits, and these go to memory through shared memory, 16 bytes a lane.
 //
 // Measured on one MI355X, whose matrix units reach 3.5e15 operations/s on random bytes (they, too, lower the clock):
-//   8,191 tokens x 2,048 into 100,260 bfloat16   1,620 to 1,710 us by the card, 2.0e15/s; 8,192 x 4,096 into 32,768 940 to 1,005 us, 2.3e15/s
+//   8,191 tokens x 2,048 into 100,260 bfloat16   1,620 to 1,760 us by the card, 1.9e15 to 2.1e15/s; 8,192 x 4,096 into 32,768 940 to 1,005 us, 2.3e15/s
 //   (torch's product with 32-bit sums written: 2,008 and 1,017 us)
+//   the same into 32-bit logits                   1,965 us, of which their 3.3 GB are 660 at 5 TB/s
 //   8 tokens x 4,096 into 100,260                 70 us, 5.9 TB/s: the reading of the weights; 32 x 8,192 into 50,000 71 us, 5.7 TB/s
 // What the first of these spent at 1,700, by leaving parts out: products and readings of shared memory alone 1,130 us, with the stages' transfers
 // (13 GB through the second-level caches, 960 us alone) 1,380, with the conversion of the logits 1,500, the rest their stores; rows of
